@@ -309,6 +309,89 @@ int feat_mean_var(AugCtx *ctx, const float *feats_dev, const int *frame_counts_d
 int aug_bucket_by_length(const int *lengths_host, int B, int batch, int *perm_host,
                          int *batch_max_host);
 
+/* -------------------------------------------------------------- rows for a model's matrix products
+ * (additions of this library; the paper stops at the features)
+ *
+ * Operators on the rows of a padded batch, of any width D: features, stacks of them, and what a
+ * model's first layers make of them.  Shared by all:
+ *   - Rows lie one behind the other, [B][T_max][D].  Row t of utterance b holds values where
+ *     t < frame_counts[b]; frame_counts_dev may be NULL: all rows do.  The other rows are not read,
+ *     and receive pad_value, or zeros where codes or gradients are written.
+ *   - Rows are fp32 or bf16 (AugElem) and aligned to their element; 16-byte aligned rows whose width
+ *     is a multiple of 8 are read and written with 128-bit accesses and are faster.
+ *   - B * T_max <= AUG_MAX_ROWS, else AUG_ECAP.  An output may be the very buffer of an input of the
+ *     same type where that is said; buffers that overlap in any other way give undefined results.
+ *   - They use no workspace of the context: calls on different contexts, and graphs captured from
+ *     them, share nothing but the caller's buffers.
+ *
+ * Microscaled rows (the OCP formats MXFP8 with e4m3 elements, and MXFP4): 32 neighbours of a row
+ * share a scale, 2^(byte - 127).  A row's elements are padded with zeros to whole groups of 128:
+ *   codes   feat_mx_code_bytes(type, D) a row: 128 (8 bits) or 64 (4 bits; the lower-numbered of two
+ *           elements in the lower half of the byte) a group
+ *   scales  feat_mx_scale_bytes(D) a row: 4 a group
+ * both 16-byte aligned, rows one behind the other.  A block's scale is 2^(floor(log2 a) - e), a its
+ * largest magnitude and e the exponent of the largest element (8 for e4m3's 448, 2 for e2m1's 6), no
+ * smaller than 2^-127; elements are rounded to nearest, ties to even, and saturate.  The scale byte of
+ * a block of zeros is 0, that of a block with a NaN or an infinity 255 (the block reads as NaN). */
+typedef enum {
+    AUG_ELEM_F32 = 0,
+    AUG_ELEM_BF16 = 1,
+    AUG_ELEM_MX8 = 2, /* microscaled e4m3 */
+    AUG_ELEM_MX4 = 3  /* microscaled e2m1 */
+} AugElem;
+#define AUG_MAX_ROWS (1 << 30)
+#define AUG_MAX_NORM_WIDTH 16384
+
+/* Host only.  Bytes of a row's codes (mx_type AUG_ELEM_MX8 or AUG_ELEM_MX4) and scales; a negative
+ * AugStatus for a bad argument. */
+int64_t feat_mx_code_bytes(int mx_type, int D);
+int64_t feat_mx_scale_bytes(int D);
+
+/* Root-mean-square norm of each row, with the addition of a residual stream:
+ *   h = x + residual,   y = h / sqrt(mean(h^2) + eps) * weight
+ * in fp32 whatever the types.
+ *   x_dev, residual_dev (or NULL), sum_dev (or NULL; receives h)   in_type
+ *   weight_dev [D] fp32, or NULL for ones
+ *   y_dev   y_type: AUG_ELEM_F32 or AUG_ELEM_BF16, [B][T_max][D], or microscaled codes, with scales_dev
+ *           (NULL otherwise)
+ * eps > 0; D <= AUG_MAX_NORM_WIDTH, else AUG_ECAP.  sum_dev may be x_dev or residual_dev, and y_dev may be
+ * either (where y_type is in_type and it is not sum_dev). */
+int feat_rms_norm(AugCtx *ctx, const void *x_dev, const void *residual_dev, int in_type,
+                  const float *weight_dev, const int *frame_counts_dev, int B, int T_max, int D, float eps,
+                  void *sum_dev, void *y_dev, int y_type, uint8_t *scales_dev);
+
+/* Its gradients.  h_dev is the sum that the norm was taken of, dy_dev the gradient of y, dsum_dev (or NULL)
+ * the gradient that reaches h by other ways; all of them, and dx_dev, of `type`.  With r = 1 / sqrt(mean(h^2) + eps):
+ *   dx = r (weight dy - h r^2 mean(weight dy h)) + dsum    (of x and residual alike; rows without values: 0)
+ *   dweight[D] = sum over all rows that hold values of dy h r, fp32, always written
+ *   partial_dev   feat_rms_norm_partial_floats(D) floats for the call's use
+ * The additions have a fixed order: the same inputs give the same bits.  dx_dev may be h_dev, dy_dev or dsum_dev.
+ * Squares are summed in fp32 without scaling: |h| < 1e17. */
+int feat_rms_norm_grad(AugCtx *ctx, const void *h_dev, const void *dy_dev, const void *dsum_dev, int type,
+                       const float *weight_dev, const int *frame_counts_dev, int B, int T_max, int D,
+                       float eps, void *dx_dev, float *dweight_dev, float *partial_dev);
+int64_t feat_rms_norm_partial_floats(int D);
+
+/* Rows to microscaled codes (codes_dev, scales_dev) and back (x_dev of out_type, exactly the numbers that the
+ * codes stand for, rounded where bf16 cannot hold them).  Weights are rows as well: B = 1, T_max = N, no
+ * frame counts. */
+int feat_mx_quantize(AugCtx *ctx, const void *x_dev, int in_type, const int *frame_counts_dev, int B,
+                     int T_max, int D, uint8_t *codes_dev, int mx_type, uint8_t *scales_dev);
+int feat_mx_dequantize(AugCtx *ctx, const uint8_t *codes_dev, int mx_type, const uint8_t *scales_dev,
+                       const int *frame_counts_dev, int B, int T_max, int D, void *x_dev, int out_type);
+
+/* A layer over the rows: out = A W^T + bias for every row that holds values, in fp32, rounded once to out_type.
+ *   a_codes_dev, a_scales_dev   rows of width K of a_type (AUG_ELEM_MX8 or AUG_ELEM_MX4), as feat_mx_quantize or
+ *                               feat_rms_norm write them
+ *   w_codes_dev, w_scales_dev   N rows of width K, AUG_ELEM_MX4: quantised once, kept by the caller
+ *   bias_dev [N] fp32 or NULL;  out_dev [B][T_max][N] of out_type (AUG_ELEM_F32 or AUG_ELEM_BF16)
+ * K and N up to AUG_MAX_PRODUCT_WIDTH, else AUG_ECAP.  Codes and scales beyond K, up to the whole group, have to be
+ * there and zero.  Products within a block are exact; sums over blocks are carried in fp32. */
+#define AUG_MAX_PRODUCT_WIDTH 16384
+int feat_mx_product(AugCtx *ctx, const uint8_t *a_codes_dev, int a_type, const uint8_t *a_scales_dev,
+                    const uint8_t *w_codes_dev, const uint8_t *w_scales_dev, const float *bias_dev,
+                    const int *frame_counts_dev, int B, int T_max, int K, int N, void *out_dev, int out_type);
+
 /* -------------------------------------------------------------- steps 1-4
  * The whole path for a batch.  Arguments as above; additionally
  *   lengths_host  the same lengths in host memory (may be NULL): used only to size

@@ -18,13 +18,16 @@ LIB_PATH = os.path.join(_HERE, "libaugb200.so")
 AUG_OK, AUG_EINVAL, AUG_ECAP, AUG_ECUDA, AUG_EPARAM, AUG_ENOMEM = 0, -1, -2, -3, -4, -5
 COMPRESS_LOG, COMPRESS_POW_1_15 = 0, 1
 LATTICE_TOTAL, LATTICE_CUBE = 0, 1
+ELEM_F32, ELEM_BF16, ELEM_MX8, ELEM_MX4 = 0, 1, 2, 3
 
 EXPORTS = ["aug_strerror", "aug_frame_count", "aug_workspace_bytes", "aug_validate_params",
            "aug_create", "aug_destroy", "aug_last_status", "aug_rir_image_method",
            "aug_reverb_mix", "feat_stft_power", "feat_vtlp_logmel", "aug_pipeline",
            "aug_pipeline_host", "aug_enable_stage_timing", "aug_stage_times", "aug_launch_count",
            "aug_measure_fp32_peak", "feat_vtlp_logmel_noalloc", "aug_last_host_bytes", "aug_upload_noise_bank", "aug_hold_parking_slots", "aug_sample_params", "feat_mfcc", "feat_mean_var",
-           "aug_bucket_by_length", "aug_vtlp_resynth"]
+           "aug_bucket_by_length", "aug_vtlp_resynth", "feat_mx_code_bytes", "feat_mx_scale_bytes",
+           "feat_rms_norm", "feat_rms_norm_grad", "feat_rms_norm_partial_floats", "feat_mx_quantize",
+           "feat_mx_dequantize", "feat_mx_product"]
 NOALLOC_MAX_BATCH = 256
 N_STAGES = 7
 STAGE_NAMES = ["rir_image", "rir_spectra", "mel_tables", "block_spectra", "convolve", "mix",
@@ -115,6 +118,23 @@ def lib() -> ctypes.CDLL:
         L.feat_mean_var.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp]
         L.aug_bucket_by_length.restype = i32
         L.aug_bucket_by_length.argtypes = [vp, i32, i32, vp, vp]
+        L.feat_mx_code_bytes.restype = i64
+        L.feat_mx_code_bytes.argtypes = [i32, i32]
+        L.feat_mx_scale_bytes.restype = i64
+        L.feat_mx_scale_bytes.argtypes = [i32]
+        L.feat_rms_norm_partial_floats.restype = i64
+        L.feat_rms_norm_partial_floats.argtypes = [i32]
+        f32 = ctypes.c_float
+        L.feat_rms_norm.restype = i32
+        L.feat_rms_norm.argtypes = [vp, vp, vp, i32, vp, vp, i32, i32, i32, f32, vp, vp, i32, vp]
+        L.feat_rms_norm_grad.restype = i32
+        L.feat_rms_norm_grad.argtypes = [vp, vp, vp, vp, i32, vp, vp, i32, i32, i32, f32, vp, vp, vp]
+        L.feat_mx_quantize.restype = i32
+        L.feat_mx_quantize.argtypes = [vp, vp, i32, vp, i32, i32, i32, vp, i32, vp]
+        L.feat_mx_dequantize.restype = i32
+        L.feat_mx_dequantize.argtypes = [vp, vp, i32, vp, vp, i32, i32, i32, vp, i32]
+        L.feat_mx_product.restype = i32
+        L.feat_mx_product.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, i32]
         L.aug_sample_params.restype = i32
         L.aug_sample_params.argtypes = [ctypes.c_uint64, ctypes.POINTER(AugDist), i32, vp, vp]
         L.aug_hold_parking_slots.restype = i32
@@ -199,6 +219,21 @@ def aug_measure_fp32_peak(stream: Optional[int] = None) -> float:
     return float(out.value)
 
 
+def feat_mx_code_bytes(mx_type: int, D: int) -> int:
+    """Bytes of a row of D microscaled codes (ELEM_MX8 or ELEM_MX4)."""
+    return _size(lib().feat_mx_code_bytes(int(mx_type), int(D)), "feat_mx_code_bytes")
+
+
+def feat_mx_scale_bytes(D: int) -> int:
+    """Bytes of a row's scales."""
+    return _size(lib().feat_mx_scale_bytes(int(D)), "feat_mx_scale_bytes")
+
+
+def feat_rms_norm_partial_floats(D: int) -> int:
+    """Floats that feat_rms_norm_grad needs for its own use."""
+    return _size(lib().feat_rms_norm_partial_floats(int(D)), "feat_rms_norm_partial_floats")
+
+
 def feat_vtlp_logmel_noalloc(config: AugConfig, power_dev, counts_dev, table_dev, B: int,
                              T_max: int, feats_dev, stream: Optional[int] = None,
                              check: bool = True) -> int:
@@ -229,6 +264,12 @@ def _ptr(t) -> Optional[int]:
 def _check(rc: int, what: str):
     if rc != AUG_OK:
         raise AugError(int(rc), what)
+
+
+def _size(n: int, what: str) -> int:
+    if n < 0:
+        raise AugError(int(n), what)
+    return int(n)
 
 
 def table_to_device(table: np.ndarray, device="cuda"):
@@ -334,6 +375,39 @@ class AugContext:
         return self._ret(lib().feat_mean_var(self._h, _ptr(feats_dev), _ptr(counts_dev), int(B),
                                              int(T_max), int(D), _ptr(mean_dev), _ptr(var_dev)),
                          "feat_mean_var", check)
+
+    def feat_rms_norm(self, x_dev, residual_dev, in_type, weight_dev, counts_dev, B, T_max, D, eps, sum_dev,
+                      y_dev, y_type, scales_dev=None, check=True):
+        return self._ret(lib().feat_rms_norm(self._h, _ptr(x_dev), _ptr(residual_dev), int(in_type),
+                                             _ptr(weight_dev), _ptr(counts_dev), int(B), int(T_max), int(D),
+                                             float(eps), _ptr(sum_dev), _ptr(y_dev), int(y_type),
+                                             _ptr(scales_dev)), "feat_rms_norm", check)
+
+    def feat_rms_norm_grad(self, h_dev, dy_dev, dsum_dev, type, weight_dev, counts_dev, B, T_max, D, eps,
+                           dx_dev, dweight_dev, partial_dev, check=True):
+        return self._ret(lib().feat_rms_norm_grad(self._h, _ptr(h_dev), _ptr(dy_dev), _ptr(dsum_dev), int(type),
+                                                  _ptr(weight_dev), _ptr(counts_dev), int(B), int(T_max),
+                                                  int(D), float(eps), _ptr(dx_dev), _ptr(dweight_dev),
+                                                  _ptr(partial_dev)), "feat_rms_norm_grad", check)
+
+    def feat_mx_quantize(self, x_dev, in_type, counts_dev, B, T_max, D, codes_dev, mx_type, scales_dev,
+                         check=True):
+        return self._ret(lib().feat_mx_quantize(self._h, _ptr(x_dev), int(in_type), _ptr(counts_dev), int(B),
+                                                int(T_max), int(D), _ptr(codes_dev), int(mx_type),
+                                                _ptr(scales_dev)), "feat_mx_quantize", check)
+
+    def feat_mx_dequantize(self, codes_dev, mx_type, scales_dev, counts_dev, B, T_max, D, x_dev, out_type,
+                           check=True):
+        return self._ret(lib().feat_mx_dequantize(self._h, _ptr(codes_dev), int(mx_type), _ptr(scales_dev),
+                                                  _ptr(counts_dev), int(B), int(T_max), int(D), _ptr(x_dev),
+                                                  int(out_type)), "feat_mx_dequantize", check)
+
+    def feat_mx_product(self, a_codes_dev, a_type, a_scales_dev, w_codes_dev, w_scales_dev, bias_dev, counts_dev,
+                        B, T_max, K, N, out_dev, out_type, check=True):
+        return self._ret(lib().feat_mx_product(self._h, _ptr(a_codes_dev), int(a_type), _ptr(a_scales_dev),
+                                               _ptr(w_codes_dev), _ptr(w_scales_dev), _ptr(bias_dev),
+                                               _ptr(counts_dev), int(B), int(T_max), int(K), int(N),
+                                               _ptr(out_dev), int(out_type)), "feat_mx_product", check)
 
     def aug_pipeline(self, speech_dev, speech_stride, lengths_dev, lengths_host, bank_dev,
                      bank_len, table_dev, B, feats_dev, T_max, counts_dev, wave_out_dev=None,
