@@ -35,7 +35,7 @@ constexpr int HOST_CHUNKS = AUG_HOST_CHUNKS;   // pipeline depth of aug_pipeline
 //   ROUTE_STORED      longer: partitions of 8192 taps, block spectra stored once and reused
 enum Route { ROUTE_FUSED_8192 = 1, ROUTE_STORED = 2 };
 
-enum Reason { R_NONE = 0, R_NSRC = 1, R_ORDER = 2, R_NOISE = 3 };
+enum Reason { R_NONE = 0, R_NSRC = 1, R_ORDER = 2, R_NOISE = 3, R_WAIT = 4 };
 
 // Per-bin entry of the warped filterbank: the bin lies in edge interval `seg`
 // (between edges e_seg and e_seg+1), at fraction `up` from its lower edge.
