@@ -9,7 +9,7 @@ SOURCES = ["api.cu", "rir.cu", "conv.cu", "feat.cu", "peak.cu", "sample.cu", "po
            "rows.cu", "product.cu"]
 HEADERS = ["common.cuh", "fft_pair.cuh", "image_delay.cuh", "mx.cuh", os.path.join("..", "..", "include", "aug_b200.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared", "-cudart", "static"]
+              "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-t", "0"]
 
 
 def _stale() -> bool:

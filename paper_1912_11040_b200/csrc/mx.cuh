@@ -16,11 +16,11 @@ constexpr int EMAX_E4M3 = 8, EMAX_E2M1 = 2;      // exponents of the formats' la
 inline __host__ __device__ int groups(int D) { return (int)(((unsigned)D + GROUP - 1) / GROUP); }
 
 #ifdef __CUDACC__
-// The scale byte of a block whose largest magnitude has these bits: floor(log2) less the format's largest exponent,
+// The scale byte of a block with this largest magnitude: floor(log2) less the format's largest exponent,
 // plus 127; 0 where that falls below it (and for a block of zeros), 255 = NaN where the block is not finite.  All of
 // it is exact, so that every way of quantising the same values gives the same codes.
-__device__ __forceinline__ unsigned scale_byte(unsigned amax_bits, int emax) {
-    const int e = (int)(amax_bits >> 23);
+__device__ __forceinline__ unsigned scale_byte(float amax, int emax) {
+    const int e = (int)(__float_as_uint(amax) >> 23 & 255u);
     return e == 255 ? 255u : (unsigned)max(e - emax, 0);
 }
 // 2^(127 - byte), by which the values are multiplied before they are rounded; 0 for a block that is not finite (its
@@ -32,7 +32,17 @@ __device__ __forceinline__ float scale_value(unsigned byte) {
     return byte == 0 ? __uint_as_float(0x00400000u) : byte == 255u ? __uint_as_float(0x7fffffffu)
                                                                    : __uint_as_float(byte << 23);
 }
-__device__ __forceinline__ unsigned abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// The larger magnitude; NaN where one is.
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 
 // Rounding to nearest, ties to even; beyond the largest number that number.
 __device__ __forceinline__ unsigned pack4_e4m3(float a, float b, float c, float d) {
@@ -62,6 +72,13 @@ __device__ __forceinline__ float2 unpack2_e4m3(unsigned short c) {
     unsigned h;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(c));
     return halves(h);
+}
+__device__ __forceinline__ void unpack4_e4m3(unsigned c, float *v) {
+    const float2 a = unpack2_e4m3((unsigned short)(c & 0xffffu)), b = unpack2_e4m3((unsigned short)(c >> 16));
+    v[0] = a.x;
+    v[1] = a.y;
+    v[2] = b.x;
+    v[3] = b.y;
 }
 // the eight elements of a word
 __device__ __forceinline__ void unpack8_e2m1(unsigned c, float *v) {
@@ -120,8 +137,10 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float *v) {
     *reinterpret_cast<uint4 *>(p) = make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]),
                                                pack2_bf16(v[6], v[7]));
 }
-__device__ __forceinline__ float load1(const float *p) { return *p; }
-__device__ __forceinline__ float load1(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float as_float(float v) { return v; }
+__device__ __forceinline__ float as_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ float load1(const T *p) { return as_float(*p); }
 __device__ __forceinline__ void store1(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 #endif
@@ -129,18 +148,25 @@ __device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float
 }  // namespace mx
 
 // The padded batch that the operators on rows share: row r is frame r % T_max of utterance r / T_max, and holds
-// values where that is below the utterance's frame count (NULL: everywhere).
+// values where that is below the utterance's frame count (NULL: everywhere).  Row numbers are below 2^30; they are
+// divided by T_max with one multiplication: floor(2^(31 + s) / T) + 1 with s the bits of T - 1, good below 2^31.
 struct RowBatch {
     const int *counts;
     int T_max;
     int rows;              // B * T_max
-    Divisor by_T;
-    RowBatch(const int *c, int T, int B) : counts(c), T_max(T), rows(B * T), by_T(T) {}
+    unsigned mul;
+    int shift;
+    RowBatch(const int *c, int T, int B) : counts(c), T_max(T), rows(B * T), shift(0) {
+        while (shift < 31 && (1u << shift) < (unsigned)T) ++shift;
+        mul = T == 1 ? 0 : (unsigned)((1ull << (31 + shift)) / (unsigned)T + 1);
+        --shift;
+    }
 #ifdef __CUDACC__
+    __device__ __forceinline__ int utterance(int row) const { return mul ? (int)(__umulhi((unsigned)row, mul) >> shift) : row; }
     __device__ __forceinline__ bool holds(int row) const {
         if (row >= rows) return false;
         if (!counts) return true;
-        const int b = by_T.of(row);
+        const int b = utterance(row);
         return row - b * T_max < counts[b];
     }
 #endif

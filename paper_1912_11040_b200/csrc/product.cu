@@ -299,7 +299,7 @@ __device__ void load_weights(const ProductArgs &p, const TilePlan &t, char *smem
 __device__ bool tile_holds(const RowBatch &batch, int m0) {
     if (!batch.counts) return true;
     const int end = min(m0 + TILE_M, batch.rows);
-    int b = batch.by_T.of(m0), t = m0 - b * batch.T_max;
+    int b = batch.utterance(m0), t = m0 - b * batch.T_max;
     for (int at = m0; at < end; at = (++b) * batch.T_max, t = 0)
         if (t < batch.counts[b]) return true;
     return false;
