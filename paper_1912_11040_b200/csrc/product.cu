@@ -145,34 +145,37 @@ int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, bo
 // multiprocessor works through a contiguous part of the tiles, ordered by columns first, so that it loads weights once
 // or twice and all CTAs pass the same rows at about the same time (they come from L2 after the first).
 //
-//   warp 0     fetches 128 rows x 128 bytes a stage with TMA, swizzled as the tensor cores read them
-//   warp 1     issues: scales of a stage from shared to tensor memory, then its multiplications
-//   warps 2-5  fetch the scales of the rows stage by stage, and the weights and their scales when the columns change
-//   warps 6-9  take finished tiles out of tensor memory (two accumulators: one fills while the other empties), add the
-//              bias, round, and write whole 128-byte lines through shared memory
+//   warp 0      fetches 128 rows x 128 bytes a stage with TMA, swizzled as the tensor cores read them, and the weights
+//               when the columns change
+//   warp 1      issues: scales of a stage from shared to tensor memory, then its multiplications
+//   warps 2-5   fetch the scales: the rows' stage by stage, the weights' when the columns change
+//   warps 6-13  take finished tiles out of tensor memory (two accumulators: one fills while the other empties), add the
+//               bias, round, and send 32 rows of 128 bytes at a time off by TMA, or write them where a row's stride
+//               or a tile's end does not allow that
 //
 // 4-bit rows multiply in 4 bits (64 of K an instruction, 256 a stage); 8-bit rows multiply in 8 bits (32 and 128), for
-// which the weights are unpacked to e4m3, of which e2m1 is a part, when they are put into shared memory.
-constexpr int TILE_M = 128, MAX_NT = 224, TILE_THREADS = 320;
+// which warps 2-5 unpack the weights to e4m3, of which e2m1 is a part, when they put them into shared memory.
+constexpr int TILE_M = 128, MAX_NT = 224, TILE_THREADS = 448;
 constexpr int STAGE_A = TILE_M * 128, STAGE_SCALES = 1024;
 constexpr int ACC_COLUMNS = MAX_NT, SCALE_COLUMNS = 2 * MAX_NT, TMEM_COLUMNS = 512;
 constexpr int LIVE_UNITS = 4096;         // tiles of a CTA that are checked for rows with values; later ones count as such
-constexpr int MAX_STAGES = 8;
-constexpr int LOADERS = 128, SCALE_LAG = 2;
+constexpr int MAX_STAGES = 8, MAX_KS = 64;
+constexpr int LOADERS = 128, SCALE_LAG = 2, WRITERS = 8, WRITER_BYTES = 4096;
 
 struct TilePlan {
     int NT, KS, stages;                  // columns of a tile, stages along K, depth of the ring
     int MT, units;                       // row tiles, tiles
     int sfb_group;                       // bytes of a group's weight scales: 512 for up to 128 columns, else 1024
     int off_sfb, off_a, off_sfa, off_out, off_misc, smem;
+    bool by_tma;                         // the output's rows can be written by TMA
 };
 
 struct TileBars {
     unsigned long long a_full[MAX_STAGES], s_full[MAX_STAGES], empty[MAX_STAGES];
-    unsigned long long b_full, b_free, acc_full[2], acc_free[2], drained;
+    unsigned long long b_full[MAX_KS], bs_full, b_free, acc_full[2], acc_free[2], drained;
     unsigned tmem;
     int dead;                            // a wait ran out: every role ends
-    float bias[4][MAX_NT];               // a copy a warp
+    float bias[WRITERS][MAX_NT];         // a copy a warp
     unsigned live[LIVE_UNITS / 32];
 };
 
@@ -189,14 +192,15 @@ __device__ __forceinline__ bool bar_try(unsigned long long *b, unsigned parity) 
                  : "=r"(ok) : "r"(smem_at(b)), "r"(parity) : "memory");
     return ok;
 }
-// Waits for a phase, for at most about two seconds (4e9 clocks); false, in all lanes, once it or another wait of the
+constexpr long long WAIT_CLOCKS = 4000000000ll;
+// Waits for a phase, for at most about two seconds; false, in all lanes, once it or another wait of the
 // CTA has run out.
 __device__ __noinline__ bool bar_wait_long(unsigned long long *b, unsigned parity, int *dead) {
     const long long t0 = clock64();
     for (;;) {
         if (bar_try(b, parity)) return true;
         if (*reinterpret_cast<volatile int *>(dead)) return false;
-        if (clock64() - t0 > 4000000000ll) {
+        if (clock64() - t0 > WAIT_CLOCKS) {
             *reinterpret_cast<volatile int *>(dead) = 1;
             return false;
         }
@@ -236,21 +240,34 @@ __device__ __forceinline__ void commit(unsigned long long *b) {
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// 32 columns of the warp's 32 lanes
-__device__ __forceinline__ void tmem_load32(unsigned at, float *v) {
-    unsigned r[32];
+// 32 columns of the warp's 32 lanes; there once tmem_loaded() has returned
+__device__ __forceinline__ void tmem_load32(unsigned at, unsigned *r) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
-        "tcgen05.wait::ld.sync.aligned;"
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
           "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(at) : "memory");
+}
+// (the registers pass through, so that nothing reads them before)
+__device__ __forceinline__ void tmem_loaded(unsigned *r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
+}
+__device__ __forceinline__ void tma_load(void *to, const CUtensorMap *map, int x, int y, unsigned long long *bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                     smem_at(to)), "l"(map), "r"(x), "r"(y), "r"(smem_at(bar)) : "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, const void *from) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];\n"
+                 "cp.async.bulk.commit_group;" ::"l"(map), "r"(x), "r"(y), "r"(smem_at(from)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(unsigned long long *b, unsigned bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(b)), "r"(bytes) : "memory");
 }
 
 // 16 bytes of e2m1 codes (32 of them) as e4m3: the same numbers by a table of eight, and the signs
@@ -263,35 +280,48 @@ __device__ __forceinline__ void e2m1_to_e4m3(unsigned c, unsigned &lo, unsigned 
     hi = __byte_perm(0x3C383000u, 0x4C484440u, i >> 16) | (s_hi & 0x80808080u);
 }
 
-// NT columns of W, all of K, and their scales into shared memory, by the loaders
-template <bool A4>
-__device__ void load_weights(const ProductArgs &p, const TilePlan &t, char *smem, int n0, int tid) {
-    // 16-byte pieces of a row's codes: 4 a group
-    const int pieces = 4 * p.G, total = t.NT * pieces;
-    for (int i = tid; i < total; i += LOADERS) {
-        const int r = i / pieces, c = i - r * pieces, n = n0 + r;
-        uint4 q = make_uint4(0, 0, 0, 0);
-        if (n < p.N) q = __ldg(reinterpret_cast<const uint4 *>(p.w + (int64_t)n * p.G * 64) + c);
-        if constexpr (A4) {                              // eight pieces to a stage's row
-            char *at = smem + (int64_t)(c >> 3) * t.NT * 128 + r * 128;
-            *reinterpret_cast<uint4 *>(at + (((c & 7) ^ (r & 7)) << 4)) = q;
-        } else {                                         // four, each of which becomes two
-            uint4 a, b;
-            e2m1_to_e4m3(q.x, a.x, a.y);
-            e2m1_to_e4m3(q.y, a.z, a.w);
-            e2m1_to_e4m3(q.z, b.x, b.y);
-            e2m1_to_e4m3(q.w, b.z, b.w);
-            char *at = smem + (int64_t)(c >> 2) * t.NT * 128 + r * 128;
-            const int j = 2 * (c & 3);
-            *reinterpret_cast<uint4 *>(at + ((j ^ (r & 7)) << 4)) = a;
-            *reinterpret_cast<uint4 *>(at + (((j + 1) ^ (r & 7)) << 4)) = b;
+// Scales of NT columns of W, all of K, by the loaders: eight groups of two columns a thread at a time
+__device__ __forceinline__ void load_weight_scales(const ProductArgs &p, const TilePlan &t, char *smem, int n0, int lt) {
+    for (int g0 = 0; g0 < p.G; g0 += 8) {
+        unsigned s[2][8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = lt + LOADERS * h, n = n0 + r;
+            const unsigned *from = reinterpret_cast<const unsigned *>(p.w_scales) + (int64_t)n * p.G + g0;
+#pragma unroll
+            for (int g = 0; g < 8; ++g) s[h][g] = r < t.NT && n < p.N && g0 + g < p.G ? __ldg(from + g) : 0u;
         }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int g = 0; g < 8; ++g)
+                if (g0 + g < p.G && 512 * h < t.sfb_group)
+                    *reinterpret_cast<unsigned *>(smem + t.off_sfb + (g0 + g) * t.sfb_group + 512 * h + (lt & 31) * 16 +
+                                                  (lt >> 5) * 4) = s[h][g];
     }
-    const int padded = t.sfb_group / 4;                  // 128 or 256 columns
-    for (int i = tid; i < padded * p.G; i += LOADERS) {
-        const int g = i / padded, r = i - g * padded, n = n0 + r;
-        const unsigned s = r < t.NT && n < p.N ? __ldg(reinterpret_cast<const unsigned *>(p.w_scales + (int64_t)n * p.G * 4) + g) : 0u;
-        *reinterpret_cast<unsigned *>(smem + t.off_sfb + g * t.sfb_group + (r >> 7) * 512 + (r & 31) * 16 + ((r >> 5) & 3) * 4) = s;
+}
+// One group of 128 of K of NT columns of W, unpacked to e4m3: read, and put into shared memory
+constexpr int UNPACKED = MAX_NT * 4 / LOADERS;           // pieces of 16 bytes a thread, four to a column
+__device__ __forceinline__ void read_weights(const ProductArgs &p, const TilePlan &t, int n0, int g, int lt, uint4 *q) {
+#pragma unroll
+    for (int i = 0; i < UNPACKED; ++i) {
+        const int r = (lt + LOADERS * i) >> 2, n = n0 + r;
+        q[i] = r < t.NT && n < p.N && g < p.G ? __ldg(reinterpret_cast<const uint4 *>(p.w + ((int64_t)n * p.G + g) * 64) + (lt & 3))
+                                              : make_uint4(0, 0, 0, 0);
+    }
+}
+__device__ __forceinline__ void put_weights(const TilePlan &t, char *to, int lt, const uint4 *q) {
+#pragma unroll
+    for (int i = 0; i < UNPACKED; ++i) {
+        const int r = (lt + LOADERS * i) >> 2, j = 2 * (lt & 3);
+        if (r >= t.NT) break;
+        uint4 a, b;
+        e2m1_to_e4m3(q[i].x, a.x, a.y);
+        e2m1_to_e4m3(q[i].y, a.z, a.w);
+        e2m1_to_e4m3(q[i].z, b.x, b.y);
+        e2m1_to_e4m3(q[i].w, b.z, b.w);
+        *reinterpret_cast<uint4 *>(to + r * 128 + ((j ^ (r & 7)) << 4)) = a;
+        *reinterpret_cast<uint4 *>(to + r * 128 + (((j + 1) ^ (r & 7)) << 4)) = b;
     }
 }
 
@@ -307,7 +337,8 @@ __device__ bool tile_holds(const RowBatch &batch, int m0) {
 
 template <bool A4>
 __global__ void __launch_bounds__(TILE_THREADS, 1)
-tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const ProductArgs p, const RowBatch batch, const TilePlan t,
+tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap w_map,
+                    const __grid_constant__ CUtensorMap out_map, const ProductArgs p, const RowBatch batch, const TilePlan t,
                     int *status) {
     extern __shared__ __align__(1024) char smem_raw[];
     char *smem = smem_raw + ((1024 - (smem_at(smem_raw) & 1023)) & 1023);
@@ -321,11 +352,12 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const ProductArgs
             bar_init(&bars->s_full[s], LOADERS / 32);
             bar_init(&bars->empty[s], 1);
         }
-        bar_init(&bars->b_full, LOADERS / 32);
+        for (int s = 0; s < t.KS; ++s) bar_init(&bars->b_full[s], A4 ? 1 : LOADERS / 32);
+        bar_init(&bars->bs_full, LOADERS / 32);
         bar_init(&bars->b_free, 1);
         for (int i = 0; i < 2; ++i) {
             bar_init(&bars->acc_full[i], 1);
-            bar_init(&bars->acc_free[i], 4);
+            bar_init(&bars->acc_free[i], WRITERS);
         }
         bar_init(&bars->drained, 1);
         bars->dead = 0;
@@ -350,45 +382,63 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const ProductArgs
     const int S = t.stages;
     constexpr int GROUPS = A4 ? 2 : 1;                   // groups of a stage
     bool ok = true;
+    // Every role goes through the CTA's tiles in the same order.  Weights are loaded for the first tile with values of
+    // each run of the same columns, `runs` counts these.
+    int n = -1, runs = 0;
 
     if (warp == 0) {
-        int slot = 0, phase = 0, issued = 0;
+        int slot = 0, phase = 0, issued = 0, weights = 0;
         for (int u = u0; u < u1 && ok; ++u) {
             if (!live(u)) continue;
             const int m0 = u % t.MT * TILE_M;
+            const bool fresh = u / t.MT != n;
+            if (fresh) {
+                n = u / t.MT;
+                if (A4 && runs && !(ok = bar_wait(&bars->b_free, (runs - 1) & 1, dead))) break;
+                ++runs;
+                weights = 0;
+            }
             for (int ks = 0; ks < t.KS; ++ks) {
+                if (A4 && fresh) {
+                    if (lane == 0) {
+                        bar_expect(&bars->b_full[ks], t.NT * 128);
+                        tma_load(smem + ks * t.NT * 128, &w_map, ks * 128, n * t.NT, &bars->b_full[ks]);
+                    }
+                    ++weights;
+                }
                 if (!(ok = bar_wait(&bars->empty[slot], phase ^ 1, dead))) break;
                 if (lane == 0) {
-                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(&bars->a_full[slot])),
-                                 "r"(STAGE_A) : "memory");
-                    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-                                     smem_at(smem + t.off_a + slot * STAGE_A)), "l"(&a_map), "r"(ks * 128), "r"(m0),
-                                 "r"(smem_at(&bars->a_full[slot])) : "memory");
+                    bar_expect(&bars->a_full[slot], STAGE_A);
+                    tma_load(smem + t.off_a + slot * STAGE_A, &a_map, ks * 128, m0, &bars->a_full[slot]);
                 }
                 ++issued;
                 if (++slot == S) slot = 0, phase ^= 1;
             }
         }
         if (!ok) {                                       // copies in flight end before the CTA does
+            const long long start = clock64();
+            for (int i = 0; i < weights; ++i)
+                while (!bar_try(&bars->b_full[i], (runs - 1) & 1) && clock64() - start < WAIT_CLOCKS) {}
             for (int i = 0; i < S && i < issued; ++i) {
                 if (--slot < 0) slot = S - 1, phase ^= 1;
-                const long long start = clock64();
-                while (!bar_try(&bars->a_full[slot], phase) && clock64() - start < 4000000000ll) {}
+                while (!bar_try(&bars->a_full[slot], phase) && clock64() - start < WAIT_CLOCKS) {}
             }
         }
     } else if (warp == 1) {
         const unsigned idesc = (A4 ? 1u << 7 | 1u << 10 : 0u) | (unsigned)(t.NT >> 3) << 17 | 1u << 23 | 1u << 27;
-        int slot = 0, phase = 0, it = 0, j = 0, runs = 0, n = -1;
+        int slot = 0, phase = 0, it = 0, j = 0;
         for (int u = u0; u < u1 && ok; ++u) {
-            if (u / t.MT != n) {                         // other columns: their weights
-                if (n >= 0 && lane == 0) commit(&bars->b_free);
-                n = u / t.MT;
-                if (!(ok = bar_wait(&bars->b_full, runs++ & 1, dead))) break;
-            }
             if (!live(u)) continue;
+            const bool fresh = u / t.MT != n;
+            if (fresh) {
+                n = u / t.MT;
+                if (runs && lane == 0) commit(&bars->b_free);
+                if (!(ok = bar_wait(&bars->bs_full, runs++ & 1, dead))) break;
+            }
             const unsigned acc = tmem + (j & 1) * ACC_COLUMNS;
             if (!(ok = bar_wait(&bars->acc_free[j & 1], ((j >> 1) & 1) ^ 1, dead))) break;
             for (int ks = 0; ks < t.KS; ++ks, ++it) {
+                if (fresh && !(ok = bar_wait(&bars->b_full[ks], (runs - 1) & 1, dead))) break;
                 if (!(ok = bar_wait(&bars->a_full[slot], phase, dead) && bar_wait(&bars->s_full[slot], phase, dead))) break;
                 tmem_fence_after();
                 if (lane == 0) {
@@ -424,34 +474,39 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const ProductArgs
         if (lane == 0) {
             commit(&bars->drained);
             const long long start = clock64();
-            while (!bar_try(&bars->drained, 0) && clock64() - start < 4000000000ll) {}
+            while (!bar_try(&bars->drained, 0) && clock64() - start < WAIT_CLOCKS) {}
         }
         __syncwarp();
         tmem_fence_before();
     } else if (warp < 6) {
         const int lt = tid - 64;
-        int slot = 0, phase = 0, n = -1, runs = 0;
+        int slot = 0, phase = 0;
         int pending = 0, done = 0;                       // stages whose scales are on their way, slot of the first of them
-        auto deliver = [&]() {
+        auto deliver = [&](unsigned long long *bar) {
             fence_async();
             __syncwarp();
-            if (lane == 0) bar_arrive(&bars->s_full[done]);
+            if (lane == 0) bar_arrive(bar);
+        };
+        auto deliver_scales = [&]() {
+            deliver(&bars->s_full[done]);
             if (++done == S) done = 0;
             --pending;
         };
         for (int u = u0; u < u1 && ok; ++u) {
-            if (u / t.MT != n) {
+            if (!live(u)) continue;
+            const bool fresh = u / t.MT != n;
+            uint4 w[UNPACKED];
+            if (fresh) {
+                // the tiles before need their scales before they are done with their weights
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
-                while (pending) deliver();
+                while (pending) deliver_scales();
                 n = u / t.MT;
                 if (runs && !(ok = bar_wait(&bars->b_free, (runs - 1) & 1, dead))) break;
                 ++runs;
-                load_weights<A4>(p, t, smem, n * t.NT, lt);
-                fence_async();
-                __syncwarp();
-                if (lane == 0) bar_arrive(&bars->b_full);
+                if (!A4) read_weights(p, t, n * t.NT, 0, lt, w);
+                load_weight_scales(p, t, smem, n * t.NT, lt);
+                deliver(&bars->bs_full);
             }
-            if (!live(u)) continue;
             const int m = u % t.MT * TILE_M + lt;
             const uint8_t *from = p.a_scales + (int64_t)min(m, batch.rows - 1) * p.G * 4;
             const unsigned bytes = m < batch.rows ? 4 : 0;
@@ -464,24 +519,35 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const ProductArgs
                         asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 512 * g),
                                      "l"(from + 4 * (ks * GROUPS + g)), "r"(bytes) : "memory");
                 asm volatile("cp.async.commit_group;" ::: "memory");
+                if (!A4 && fresh) {                      // a group of weights behind the next one's reads
+                    uint4 next[UNPACKED];
+                    read_weights(p, t, n * t.NT, ks + 1, lt, next);
+                    put_weights(t, smem + ks * t.NT * 128, lt, w);
+                    deliver(&bars->b_full[ks]);
+#pragma unroll
+                    for (int i = 0; i < UNPACKED; ++i) w[i] = next[i];
+                }
                 if (++pending > SCALE_LAG) {
                     asm volatile("cp.async.wait_group %0;" ::"n"(SCALE_LAG) : "memory");
-                    deliver();
+                    deliver_scales();
                 }
                 if (++slot == S) slot = 0, phase ^= 1;
             }
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
-        while (pending) deliver();
+        while (pending) deliver_scales();
     } else {
-        const int q = warp & 3;                          // the lanes of tensor memory that this warp may read
-        char *stage = smem + t.off_out + q * 4096;
-        float *bias = bars->bias[q];
-        int n = -1, j = 0;
-        const int size = p.bf16_out ? 2 : 4, unit = 16 / size;
+        const int q = warp & 3, half = (warp - 6) >> 2;  // the lanes of tensor memory that this warp may read; every other piece
+        char *stage = smem + t.off_out + (warp - 6) * WRITER_BYTES;
+        float *bias = bars->bias[warp - 6];
+        int j = 0;
+        const int size = p.bf16_out ? 2 : 4, unit = 16 / size, wide = 128 / size;      // a piece: 32 rows of 128 bytes
         const bool vec = (p.N & (unit - 1)) == 0 && (reinterpret_cast<uintptr_t>(p.out) & 15) == 0;
         for (int u = u0; u < u1 && ok; ++u) {
             const int n0 = u / t.MT * t.NT, row0 = u % t.MT * TILE_M + 32 * q, cols = min(t.NT, p.N - n0);
+            const int rows = min(32, batch.rows - row0);     // may be negative
+            const bool alive = live(u), valid = alive && batch.holds(row0 + lane);
+            const bool some = __any_sync(~0u, valid);
             if (u / t.MT != n) {
                 n = u / t.MT;
                 __syncwarp();
@@ -489,34 +555,32 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const ProductArgs
                 __syncwarp();
             }
             char *out = static_cast<char *>(p.out) + ((int64_t)row0 * p.N + n0) * size;
-            const int rows = min(32, batch.rows - row0);     // may be negative
-            if (!live(u)) {
-                for (int r = 0; r < rows; ++r)
-                    for (int c = lane; c < cols; c += 32) {
-                        if (p.bf16_out)
-                            reinterpret_cast<__nv_bfloat16 *>(out)[(int64_t)r * p.N + c] = __float2bfloat16_rn(p.pad);
-                        else
-                            reinterpret_cast<float *>(out)[(int64_t)r * p.N + c] = p.pad;
-                    }
-                continue;
+            if (alive) {
+                if (!(ok = bar_wait(&bars->acc_full[j & 1], (j >> 1) & 1, dead))) break;
+                tmem_fence_after();
             }
-            const bool valid = batch.holds(row0 + lane);
-            if (!(ok = bar_wait(&bars->acc_full[j & 1], (j >> 1) & 1, dead))) break;
-            tmem_fence_after();
             const unsigned acc = tmem + (j & 1) * ACC_COLUMNS + ((unsigned)q << 21);
-            const int wide = p.bf16_out ? 64 : 32;           // columns of 128 bytes
-            for (int c0 = 0; c0 < cols; c0 += wide) {
-                for (int half = 0; half < wide / 32; ++half) {
-                    const int c1 = c0 + 32 * half;
-                    if (c1 >= cols) break;
-                    float v[32];
-                    tmem_load32(acc + c1, v);
+            for (int c0 = half * wide; c0 < cols; c0 += 2 * wide) {
+                unsigned r[2][32];
+                const bool both = p.bf16_out && c0 + 32 < cols;      // 64 columns of 16 bits, 32 of 32
+                if (some) {
+                    tmem_load32(acc + c0, r[0]);
+                    if (both) tmem_load32(acc + c0 + 32, r[1]);
+                    tmem_loaded(r[0]);
+                    if (both) tmem_loaded(r[1]);
+                }
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                __syncwarp();                            // the piece before has left
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = valid ? v[i] + bias[c1 + i] : p.pad;
+                for (int h = 0; h < 2; ++h) {
+                    if (h && !both) break;
+                    float v[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = valid ? __uint_as_float(r[h][i]) + bias[c0 + 32 * h + i] : p.pad;
                     if (p.bf16_out) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            mx::store8(reinterpret_cast<__nv_bfloat16 *>(stage + lane * 128 + (((4 * half + i) ^ (lane & 7)) << 4)),
+                            mx::store8(reinterpret_cast<__nv_bfloat16 *>(stage + lane * 128 + (((4 * h + i) ^ (lane & 7)) << 4)),
                                        v + 8 * i);
                     } else {
 #pragma unroll
@@ -525,36 +589,42 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const ProductArgs
                                 make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                     }
                 }
-                if (c0 + wide >= cols) {                     // all of it has been taken
-                    tmem_fence_before();
+                if (t.by_tma && (c0 + wide <= cols || n0 + cols == p.N)) {
+                    fence_async();
                     __syncwarp();
-                    if (lane == 0) bar_arrive(&bars->acc_free[j & 1]);
-                }
-                __syncwarp();
-                if (vec) {
+                    if (lane == 0 && rows > 0) tma_store(&out_map, n0 + c0, row0, stage);
+                } else if (vec) {
+                    __syncwarp();
                     const int i = lane & 7, c = c0 + i * unit;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const int r = 4 * k + (lane >> 3);
-                        if (r < rows && c < cols)
-                            *reinterpret_cast<uint4 *>(out + ((int64_t)r * p.N + c) * size) =
-                                *reinterpret_cast<const uint4 *>(stage + r * 128 + ((i ^ (r & 7)) << 4));
+                        const int y = 4 * k + (lane >> 3);
+                        if (y < rows && c < cols)
+                            *reinterpret_cast<uint4 *>(out + ((int64_t)y * p.N + c) * size) =
+                                *reinterpret_cast<const uint4 *>(stage + y * 128 + ((i ^ (y & 7)) << 4));
                     }
                 } else {
-                    for (int r = 0; r < rows; ++r)
+                    __syncwarp();
+                    for (int y = 0; y < rows; ++y)
                         for (int c = lane; c < wide && c0 + c < cols; c += 32) {
-                            const char *from = stage + r * 128 + (((c / unit) ^ (r & 7)) << 4) + c % unit * size;
-                            char *to = out + ((int64_t)r * p.N + c0 + c) * size;
+                            const char *from = stage + y * 128 + (((c / unit) ^ (y & 7)) << 4) + c % unit * size;
+                            char *to = out + ((int64_t)y * p.N + c0 + c) * size;
                             if (p.bf16_out)
                                 *reinterpret_cast<unsigned short *>(to) = *reinterpret_cast<const unsigned short *>(from);
                             else
                                 *reinterpret_cast<float *>(to) = *reinterpret_cast<const float *>(from);
                         }
                 }
-                __syncwarp();
             }
-            ++j;
+            if (alive) {                                 // all of it has been taken
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(&bars->acc_free[j & 1]);
+                ++j;
+            }
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
         tmem_fence_before();
     }
     __syncthreads();
@@ -571,12 +641,14 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, Tile
     double least = 0;
     bool found = false;
     int last = 0;
+    if (KS > MAX_KS) return false;
     for (int tiles = (p.N + MAX_NT - 1) / MAX_NT; tiles <= (p.N + 15) / 16; ++tiles) {
         TilePlan t;
         t.NT = ((p.N + tiles - 1) / tiles + 15) / 16 * 16;
         if (t.NT == last) continue;
         last = t.NT;
         t.KS = KS;
+        t.by_tma = (int64_t)p.N * (p.bf16_out ? 2 : 4) % 16 == 0 && on16(p.out);
         t.MT = MT;
         const int64_t units = (int64_t)MT * ((p.N + t.NT - 1) / t.NT);
         if (units > INT32_MAX / 2) break;
@@ -584,12 +656,12 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, Tile
         t.sfb_group = t.NT > 128 ? 1024 : 512;
         t.off_sfb = KS * t.NT * 128;
         t.off_a = (t.off_sfb + p.G * t.sfb_group + 1023) & ~1023;
-        const int fixed = 4 * 4096 + (int)sizeof(TileBars) + 1024;
+        const int fixed = WRITERS * WRITER_BYTES + (int)sizeof(TileBars) + 1024;
         t.stages = std::min(MAX_STAGES, (ctx->smem_per_sm - 1024 - fixed - t.off_a) / (STAGE_A + STAGE_SCALES));
         if (t.stages < SCALE_LAG + 1) continue;
         t.off_sfa = t.off_a + t.stages * STAGE_A;
         t.off_out = t.off_sfa + t.stages * STAGE_SCALES;
-        t.off_misc = t.off_out + 4 * 4096;
+        t.off_misc = t.off_out + WRITERS * WRITER_BYTES;
         t.smem = t.off_misc + (int)sizeof(TileBars) + 1024;
         // rounds of tiles on the busiest multiprocessor, their columns and what every tile costs besides
         const double cost = (double)((t.units + ctx->sm_count - 1) / ctx->sm_count) * (t.NT + 32);
@@ -622,14 +694,25 @@ template <bool A4>
 int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const TilePlan &t) {
     const EncodeTiled encode = encode_tiled();
     if (!encode || smem_opt_in<tile_product_kernel<A4>>(ctx->device) != AUG_OK) return AUG_ECUDA;
-    CUtensorMap map;
-    const cuuint64_t dims[2] = {(cuuint64_t)p.G * (A4 ? 64 : 128), (cuuint64_t)batch.rows}, strides[1] = {dims[0]};
-    const cuuint32_t box[2] = {128, TILE_M}, steps[2] = {1, 1};
-    if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(p.a), dims, strides, box, steps,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    auto describe = [&](CUtensorMap *map, CUtensorMapDataType type, void *base, uint64_t width, uint64_t rows, uint64_t bytes,
+                        int box_x, int box_y) {
+        const cuuint64_t dims[2] = {width, rows}, strides[1] = {bytes};
+        const cuuint32_t box[2] = {(cuuint32_t)box_x, (cuuint32_t)box_y}, steps[2] = {1, 1};
+        return encode(map, type, 2, base, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                      CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    CUtensorMap a, w, out;
+    const uint64_t a_bytes = (uint64_t)p.G * (A4 ? 64 : 128), w_bytes = (uint64_t)p.G * 64, size = p.bf16_out ? 2 : 4;
+    if (!describe(&a, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<uint8_t *>(p.a), a_bytes, batch.rows, a_bytes, 128, TILE_M))
         return AUG_ECUDA;
-    tile_product_kernel<A4><<<std::min(t.units, ctx->sm_count), TILE_THREADS, t.smem, ctx->stream>>>(map, p, batch, t, ctx->status);
+    w = out = a;                                         // (those that are not used)
+    if (A4 && !describe(&w, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<uint8_t *>(p.w), w_bytes, p.N, w_bytes, 128, t.NT))
+        return AUG_ECUDA;
+    if (t.by_tma && !describe(&out, p.bf16_out ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.out, p.N,
+                              batch.rows, p.N * size, 128 / (int)size, 32))
+        return AUG_ECUDA;
+    tile_product_kernel<A4><<<std::min(t.units, ctx->sm_count), TILE_THREADS, t.smem, ctx->stream>>>(a, w, out, p, batch, t,
+                                                                                                     ctx->status);
     AUG_CUDA_OK(cudaGetLastError());
     ctx->launches++;
     return AUG_OK;
