@@ -16,10 +16,11 @@ struct ProductArgs {
     float pad;
 };
 
-// 2^(a + w - 254 - down) v, without overflow or underflow on the way; NaN where either byte says so
+// 2^(a + w - 254 - down) v in two steps, neither of which overflows or underflows unless the result does; NaN where either
+// byte says so
 __device__ __forceinline__ float scaled(float v, unsigned a, unsigned w, int down) {
-    const int e = (int)(a + w) - 254 - down, h = e >> 1;          // -257 .. 254
-    const float p = ldexpf(ldexpf(v, h), e - h);
+    const int e = (int)(a + w) - 254 - down, h = max(e >> 1, -126), k = max(e - h, -126);
+    const float p = v * __int_as_float((h + 127) << 23) * __int_as_float((k + 127) << 23);
     return a == 255u || w == 255u ? __uint_as_float(0x7fffffffu) : p;
 }
 
@@ -35,24 +36,21 @@ __device__ __forceinline__ uint2 twice_e2m1(unsigned c) {
 }
 
 // ---------------------------------------------------------------- few rows
-// A frame (or a few) of a stream: bound by reading the weights, half a byte each.  A lane holds a block of 32 of a
-// row's values and of each of COLS columns' weights; P lanes, a power of two, share a column.  4-bit products are
-// sums of whole numbers, four at a time (both operands doubled), exact until the block's scale is applied.
-constexpr int FEW_THREADS = 256, FEW_COLS = 4;
-constexpr int FEW_ROWS = 8;
+// A frame (or a few) of a stream: bound by reading the weights, half a byte each.  A lane holds a block of 32 of each
+// of COLS columns' weights and goes through R rows with them; P lanes, a power of two, share a column.  4-bit products
+// are sums of whole numbers, four at a time (both operands doubled), exact until the block's scale is applied.
+constexpr int FEW_THREADS = 256, FEW_COLS = 4, FEW_ROWS = 8;
 
-template <bool A4>
+template <bool A4, int R>
 __global__ void __launch_bounds__(FEW_THREADS)
 few_rows_kernel(ProductArgs p, RowBatch batch, int P) {
     const int lane = threadIdx.x & 31, part = lane & (P - 1), per_warp = 32 / P;
     const int warp = (blockIdx.x * FEW_THREADS + threadIdx.x) >> 5;
     const int n0 = (warp * per_warp + lane / P) * FEW_COLS, blocks = 4 * p.G;
-    for (int row = blockIdx.y; row < batch.rows; row += gridDim.y) {
-        float acc[FEW_COLS] = {};
-        const bool valid = batch.holds(row);
-        const uint8_t *a = p.a + (int64_t)row * p.G * (A4 ? 64 : 128);
-        for (int b = part; valid && b < blocks; b += P) {
-            const unsigned sa = p.a_scales[(int64_t)row * blocks + b];
+    for (int row0 = blockIdx.y * R; row0 < batch.rows; row0 += gridDim.y * R) {
+        const int rows = min(R, batch.rows - row0);
+        float acc[R][FEW_COLS] = {};
+        for (int b = part; b < blocks; b += P) {
             uint4 w[FEW_COLS];
             unsigned sw[FEW_COLS];
 #pragma unroll
@@ -62,76 +60,100 @@ few_rows_kernel(ProductArgs p, RowBatch batch, int P) {
                 sw[c] = __ldg(p.w_scales + (int64_t)n * blocks + b);
             }
             if constexpr (A4) {
-                const uint4 q = reinterpret_cast<const uint4 *>(a)[b];
-                const unsigned aw[4] = {q.x, q.y, q.z, q.w};
-                uint2 av[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) av[i] = twice_e2m1(aw[i]);
+                uint2 wv[FEW_COLS][4];
 #pragma unroll
                 for (int c = 0; c < FEW_COLS; ++c) {
                     const unsigned ww[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
-                    int dot = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) wv[c][i] = twice_e2m1(ww[i]);
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    if (r >= rows) break;
+                    const uint4 q = reinterpret_cast<const uint4 *>(p.a + (int64_t)(row0 + r) * p.G * 64)[b];
+                    const unsigned sa = p.a_scales[(int64_t)(row0 + r) * blocks + b], aw[4] = {q.x, q.y, q.z, q.w};
+                    int dot[FEW_COLS] = {};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const uint2 wv = twice_e2m1(ww[i]);
-                        dot = __dp4a((int)av[i].x, (int)wv.x, dot);
-                        dot = __dp4a((int)av[i].y, (int)wv.y, dot);
+                        const uint2 av = twice_e2m1(aw[i]);
+#pragma unroll
+                        for (int c = 0; c < FEW_COLS; ++c)
+                            dot[c] = __dp4a((int)av.y, (int)wv[c][i].y, __dp4a((int)av.x, (int)wv[c][i].x, dot[c]));
                     }
-                    acc[c] += scaled((float)dot, sa, sw[c], 2);
+#pragma unroll
+                    for (int c = 0; c < FEW_COLS; ++c) acc[r][c] += scaled((float)dot[c], sa, sw[c], 2);
                 }
             } else {
-                const uint4 q[2] = {reinterpret_cast<const uint4 *>(a)[2 * b], reinterpret_cast<const uint4 *>(a)[2 * b + 1]};
-                const unsigned aw[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[1].x, q[1].y, q[1].z, q[1].w};
-                float dot[FEW_COLS] = {};
+                float dot[R][FEW_COLS] = {};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float av[8];
+                for (int i = 0; i < 4; ++i) {            // eight values at a time
+                    float wv[FEW_COLS][8];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 f = mx::unpack2_e4m3((unsigned short)(aw[2 * i + (j >> 1)] >> (16 * (j & 1))));
-                        av[2 * j] = f.x;
-                        av[2 * j + 1] = f.y;
-                    }
+                    for (int c = 0; c < FEW_COLS; ++c)
+                        mx::unpack8_e2m1(i == 0 ? w[c].x : i == 1 ? w[c].y : i == 2 ? w[c].z : w[c].w, wv[c]);
 #pragma unroll
-                    for (int c = 0; c < FEW_COLS; ++c) {
-                        float wv[8];
-                        mx::unpack8_e2m1(i == 0 ? w[c].x : i == 1 ? w[c].y : i == 2 ? w[c].z : w[c].w, wv);
+                    for (int r = 0; r < R; ++r) {
+                        if (r >= rows) break;
+                        const uint2 q = reinterpret_cast<const uint2 *>(p.a + (int64_t)(row0 + r) * p.G * 128)[4 * b + i];
+                        float av[8];
+                        mx::unpack4_e4m3(q.x, av);
+                        mx::unpack4_e4m3(q.y, av + 4);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) dot[c] = fmaf(av[j], wv[j], dot[c]);
+                        for (int c = 0; c < FEW_COLS; ++c)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) dot[r][c] = fmaf(av[j], wv[c][j], dot[r][c]);
                     }
                 }
 #pragma unroll
-                for (int c = 0; c < FEW_COLS; ++c) acc[c] += scaled(dot[c], sa, sw[c], 0);
+                for (int r = 0; r < R; ++r) {
+                    if (r >= rows) break;
+                    const unsigned sa = p.a_scales[(int64_t)(row0 + r) * blocks + b];
+#pragma unroll
+                    for (int c = 0; c < FEW_COLS; ++c) acc[r][c] += scaled(dot[r][c], sa, sw[c], 0);
+                }
             }
         }
         for (int o = P >> 1; o; o >>= 1)
 #pragma unroll
-            for (int c = 0; c < FEW_COLS; ++c) acc[c] += __shfl_xor_sync(~0u, acc[c], o);
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int c = 0; c < FEW_COLS; ++c) acc[r][c] += __shfl_xor_sync(~0u, acc[r][c], o);
         if (part == 0) {
 #pragma unroll
-            for (int c = 0; c < FEW_COLS; ++c) {
-                const int n = n0 + c;
-                if (n >= p.N) break;
-                const float v = valid ? acc[c] + (p.bias ? __ldg(p.bias + n) : 0.f) : p.pad;
-                const int64_t at = (int64_t)row * p.N + n;
-                if (p.bf16_out)
-                    static_cast<__nv_bfloat16 *>(p.out)[at] = __float2bfloat16_rn(v);
-                else
-                    static_cast<float *>(p.out)[at] = v;
+            for (int r = 0; r < R; ++r) {
+                if (r >= rows) break;
+                const bool valid = batch.holds(row0 + r);
+#pragma unroll
+                for (int c = 0; c < FEW_COLS; ++c) {
+                    const int n = n0 + c;
+                    if (n >= p.N) break;
+                    const float v = valid ? acc[r][c] + (p.bias ? __ldg(p.bias + n) : 0.f) : p.pad;
+                    const int64_t at = (int64_t)(row0 + r) * p.N + n;
+                    if (p.bf16_out)
+                        static_cast<__nv_bfloat16 *>(p.out)[at] = __float2bfloat16_rn(v);
+                    else
+                        static_cast<float *>(p.out)[at] = v;
+                }
             }
         }
     }
 }
 
-int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, bool a4) {
+template <bool A4>
+int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch) {
     int P = 4;
     while (P < 32 && P < 4 * p.G) P *= 2;
     const int cols = FEW_THREADS / P * FEW_COLS;                  // of a CTA
-    const dim3 grid((p.N + cols - 1) / cols, std::min(batch.rows, 65535));
-    if (a4)
-        few_rows_kernel<true><<<grid, FEW_THREADS, 0, ctx->stream>>>(p, batch, P);
+    auto go = [&](auto kern, int R) {
+        const dim3 grid((p.N + cols - 1) / cols, std::min((batch.rows + R - 1) / R, 65535));
+        kern<<<grid, FEW_THREADS, 0, ctx->stream>>>(p, batch, P);
+    };
+    if (batch.rows == 1)
+        go(few_rows_kernel<A4, 1>, 1);
+    else if (batch.rows <= 4)
+        go(few_rows_kernel<A4, 4>, 4);
     else
-        few_rows_kernel<false><<<grid, FEW_THREADS, 0, ctx->stream>>>(p, batch, P);
+        go(few_rows_kernel<A4, FEW_ROWS>, FEW_ROWS);
     AUG_CUDA_OK(cudaGetLastError());
     ctx->launches++;
     return AUG_OK;
@@ -146,36 +168,38 @@ int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, bo
 // or twice and all CTAs pass the same rows at about the same time (they come from L2 after the first).
 //
 //   warp 0      fetches 128 rows x 128 bytes a stage with TMA, swizzled as the tensor cores read them, and the weights
-//               when the columns change
-//   warp 1      issues: scales of a stage from shared to tensor memory, then its multiplications
-//   warps 2-5   fetch the scales: the rows' stage by stage, the weights' when the columns change
+//               when the columns change;  warp 14 the rows' scales, some tiles ahead
+//   warp 1      issues the multiplications
+//   warps 2-5   put the scales into tensor memory: the rows' eight groups of 128 at a time, the weights' when the columns
+//               change
 //   warps 6-13  take finished tiles out of tensor memory (two accumulators: one fills while the other empties), add the
 //               bias, round, and send 32 rows of 128 bytes at a time off by TMA, or write them where a row's stride
 //               or a tile's end does not allow that
 //
 // 4-bit rows multiply in 4 bits (64 of K an instruction, 256 a stage); 8-bit rows multiply in 8 bits (32 and 128), for
-// which warps 2-5 unpack the weights to e4m3, of which e2m1 is a part, when they put them into shared memory.
-constexpr int TILE_M = 128, MAX_NT = 224, TILE_THREADS = 448;
-constexpr int STAGE_A = TILE_M * 128, STAGE_SCALES = 1024;
-constexpr int ACC_COLUMNS = MAX_NT, SCALE_COLUMNS = 2 * MAX_NT, TMEM_COLUMNS = 512;
+// which warps 2-5 unpack the weights to e4m3, of which e2m1 is a part, and put them into shared memory.
+constexpr int TILE_M = 128, MAX_NT = 224, TILE_THREADS = 480;
+constexpr int STAGE_A = TILE_M * 128;
+constexpr int TMEM_COLUMNS = 512;
 constexpr int LIVE_UNITS = 4096;         // tiles of a CTA that are checked for rows with values; later ones count as such
-constexpr int MAX_STAGES = 8, MAX_KS = 64;
-constexpr int LOADERS = 128, SCALE_LAG = 2, WRITERS = 8, WRITER_BYTES = 4096;
+constexpr int MAX_STAGES = 8, MAX_KS = 64, MAX_AHEAD = 4;
+constexpr int LOADERS = 128, CHUNK = 8, CHUNK_COLUMNS = 32, WRITERS = 8, PIECE = 4096, WRITER_BYTES = PIECE;
 
 struct TilePlan {
     int NT, KS, stages;                  // columns of a tile, stages along K, depth of the ring
     int MT, units;                       // row tiles, tiles
-    int sfb_group;                       // bytes of a group's weight scales: 512 for up to 128 columns, else 1024
-    int off_sfb, off_a, off_sfa, off_out, off_misc, smem;
-    bool by_tma;                         // the output's rows can be written by TMA
+    int sfb_columns;                     // tensor memory's columns for a group's weight scales: a fourth of 128 or 256
+    int ahead;                           // tiles whose scales shared memory has room for
+    int off_a, off_scales, off_out, off_misc, smem;
+    bool by_tma;                         // the output's rows can be written by TMA: they start on 16-byte boundaries
 };
 
 struct TileBars {
-    unsigned long long a_full[MAX_STAGES], s_full[MAX_STAGES], empty[MAX_STAGES];
+    unsigned long long a_full[MAX_STAGES], empty[MAX_STAGES], r_full[MAX_AHEAD], r_free[MAX_AHEAD], s_full[2], s_free[2];
     unsigned long long b_full[MAX_KS], bs_full, b_free, acc_full[2], acc_free[2], drained;
     unsigned tmem;
     int dead;                            // a wait ran out: every role ends
-    float bias[WRITERS][MAX_NT];         // a copy a warp
+    alignas(16) float bias[WRITERS][MAX_NT + 32];      // a copy a warp, and what a piece reads beyond
     unsigned live[LIVE_UNITS / 32];
 };
 
@@ -206,33 +230,33 @@ __device__ __noinline__ bool bar_wait_long(unsigned long long *b, unsigned parit
         }
     }
 }
-__device__ __forceinline__ bool bar_wait(unsigned long long *b, unsigned parity, int *dead) {
-    const bool ok = bar_try(b, parity) || bar_wait_long(b, parity, dead);
-    return __all_sync(~0u, ok);
+__device__ __forceinline__ bool bar_wait_one(unsigned long long *b, unsigned parity, int *dead) {
+    return bar_try(b, parity) || bar_wait_long(b, parity, dead);
+}
+__device__ __forceinline__ bool bar_wait(unsigned long long *b, unsigned parity, int *dead) {      // a warp's lanes together
+    return __all_sync(~0u, bar_wait_one(b, parity, dead));
+}
+// One thread of a converged warp, which issues what a single thread has to
+__device__ __forceinline__ bool elected() {
+    unsigned one;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one;
 }
 
-// Shared memory descriptor of rows of 128 bytes, swizzled in groups of eight (K-major operand)
-__device__ __forceinline__ unsigned long long operand_desc(unsigned at) {
-    return (unsigned long long)((at & 0x3ffff) >> 4) | 1ull << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61;
-}
-// of 32 x 16 bytes of scales, one behind the other
-__device__ __forceinline__ unsigned long long scales_desc(unsigned at) {
-    return (unsigned long long)((at & 0x3ffff) >> 4) | 8ull << 32 | 1ull << 46;
-}
-__device__ __forceinline__ void copy_scales(unsigned column, unsigned long long desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(column), "l"(desc) : "memory");
-}
+// Shared memory descriptor of an operand with K innermost, rows of 128 bytes that are swizzled in groups of eight: the lower
+// word holds the address in units of 16 bytes.
+constexpr unsigned OPERAND_HIGH = 64u | 1u << 14 | 2u << 29;
+__device__ __forceinline__ unsigned desc_low(unsigned at) { return at >> 4; }
 template <bool A4>
-__device__ __forceinline__ void multiply(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned sfa,
-                                         unsigned sfb, bool add) {
+__device__ __forceinline__ void multiply(unsigned d, unsigned a, unsigned b, unsigned idesc, unsigned sfa, unsigned sfb, unsigned add) {
     if constexpr (A4)
-        asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %6, 0;\n"
-                     "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
-                     "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"((unsigned)add) : "memory");
+        asm volatile("{\n.reg .pred p;\n.reg .b64 x, y;\nmov.b64 x, {%1, %7};\nmov.b64 y, {%2, %7};\nsetp.ne.u32 p, %6, 0;\n"
+                     "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], x, y, %3, [%4], [%5], p;\n}" ::"r"(d), "r"(a),
+                     "r"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(add), "n"(OPERAND_HIGH) : "memory");
     else
-        asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %6, 0;\n"
-                     "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
-                     "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"((unsigned)add) : "memory");
+        asm volatile("{\n.reg .pred p;\n.reg .b64 x, y;\nmov.b64 x, {%1, %7};\nmov.b64 y, {%2, %7};\nsetp.ne.u32 p, %6, 0;\n"
+                     "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], x, y, %3, [%4], [%5], p;\n}" ::"r"(d), "r"(a),
+                     "r"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(add), "n"(OPERAND_HIGH) : "memory");
 }
 __device__ __forceinline__ void commit(unsigned long long *b) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(b)) : "memory");
@@ -240,6 +264,21 @@ __device__ __forceinline__ void commit(unsigned long long *b) {
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_store16(unsigned at, const unsigned *r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(
+                     at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+                 "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_store32(unsigned at, const unsigned *r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+        "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
+        "r"(r[31]) : "memory");
+}
 // 32 columns of the warp's 32 lanes; there once tmem_loaded() has returned
 __device__ __forceinline__ void tmem_load32(unsigned at, unsigned *r) {
     asm volatile(
@@ -258,9 +297,20 @@ __device__ __forceinline__ void tmem_loaded(unsigned *r) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
 }
+__device__ __forceinline__ void add_pair(unsigned &a, unsigned &b, unsigned x, unsigned y) {
+    asm("{\n.reg .b64 p, q;\nmov.b64 p, {%0, %1};\nmov.b64 q, {%2, %3};\nadd.rn.f32x2 p, p, q;\nmov.b64 {%0, %1}, p;\n}"
+        : "+r"(a), "+r"(b) : "r"(x), "r"(y));
+}
+__device__ __forceinline__ unsigned pack2(const unsigned *v) {
+    return mx::pack2_bf16(__uint_as_float(v[0]), __uint_as_float(v[1]));
+}
 __device__ __forceinline__ void tma_load(void *to, const CUtensorMap *map, int x, int y, unsigned long long *bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
                      smem_at(to)), "l"(map), "r"(x), "r"(y), "r"(smem_at(bar)) : "memory");
+}
+__device__ __forceinline__ void tma_load1(void *to, const CUtensorMap *map, int x, unsigned long long *bar) {
+    asm volatile("cp.async.bulk.tensor.1d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2}], [%3];" ::"r"(
+                     smem_at(to)), "l"(map), "r"(x), "r"(smem_at(bar)) : "memory");
 }
 __device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, const void *from) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];\n"
@@ -280,26 +330,6 @@ __device__ __forceinline__ void e2m1_to_e4m3(unsigned c, unsigned &lo, unsigned 
     hi = __byte_perm(0x3C383000u, 0x4C484440u, i >> 16) | (s_hi & 0x80808080u);
 }
 
-// Scales of NT columns of W, all of K, by the loaders: eight groups of two columns a thread at a time
-__device__ __forceinline__ void load_weight_scales(const ProductArgs &p, const TilePlan &t, char *smem, int n0, int lt) {
-    for (int g0 = 0; g0 < p.G; g0 += 8) {
-        unsigned s[2][8];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = lt + LOADERS * h, n = n0 + r;
-            const unsigned *from = reinterpret_cast<const unsigned *>(p.w_scales) + (int64_t)n * p.G + g0;
-#pragma unroll
-            for (int g = 0; g < 8; ++g) s[h][g] = r < t.NT && n < p.N && g0 + g < p.G ? __ldg(from + g) : 0u;
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int g = 0; g < 8; ++g)
-                if (g0 + g < p.G && 512 * h < t.sfb_group)
-                    *reinterpret_cast<unsigned *>(smem + t.off_sfb + (g0 + g) * t.sfb_group + 512 * h + (lt & 31) * 16 +
-                                                  (lt >> 5) * 4) = s[h][g];
-    }
-}
 // One group of 128 of K of NT columns of W, unpacked to e4m3: read, and put into shared memory
 constexpr int UNPACKED = MAX_NT * 4 / LOADERS;           // pieces of 16 bytes a thread, four to a column
 __device__ __forceinline__ void read_weights(const ProductArgs &p, const TilePlan &t, int n0, int g, int lt, uint4 *q) {
@@ -337,7 +367,7 @@ __device__ bool tile_holds(const RowBatch &batch, int m0) {
 
 template <bool A4>
 __global__ void __launch_bounds__(TILE_THREADS, 1)
-tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap w_map,
+tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap s_map, const __grid_constant__ CUtensorMap w_map,
                     const __grid_constant__ CUtensorMap out_map, const ProductArgs p, const RowBatch batch, const TilePlan t,
                     int *status) {
     extern __shared__ __align__(1024) char smem_raw[];
@@ -349,17 +379,22 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
     if (tid == 0) {
         for (int s = 0; s < t.stages; ++s) {
             bar_init(&bars->a_full[s], 1);
-            bar_init(&bars->s_full[s], LOADERS / 32);
             bar_init(&bars->empty[s], 1);
+        }
+        for (int s = 0; s < t.ahead; ++s) {
+            bar_init(&bars->r_full[s], 1);
+            bar_init(&bars->r_free[s], LOADERS / 32);
         }
         for (int s = 0; s < t.KS; ++s) bar_init(&bars->b_full[s], A4 ? 1 : LOADERS / 32);
         bar_init(&bars->bs_full, LOADERS / 32);
         bar_init(&bars->b_free, 1);
-        for (int i = 0; i < 2; ++i) {
-            bar_init(&bars->acc_full[i], 1);
-            bar_init(&bars->acc_free[i], WRITERS);
-        }
         bar_init(&bars->drained, 1);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&bars->s_full[i], LOADERS / 32);
+            bar_init(&bars->s_free[i], 1);
+            bar_init(&bars->acc_full[i], 1);
+            bar_init(&bars->acc_free[i], WRITERS / 2);
+        }
         bars->dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -384,94 +419,113 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
     bool ok = true;
     // Every role goes through the CTA's tiles in the same order.  Weights are loaded for the first tile with values of
     // each run of the same columns, `runs` counts these.
+    struct Tile {
+        int u, m, n, MT;
+        __device__ __forceinline__ void next() {
+            ++u;
+            if (++m == MT) m = 0, ++n;
+        }
+    } at;
+    at.u = u0;
+    at.MT = t.MT;
+    at.n = u0 / t.MT;
+    at.m = u0 - at.n * t.MT;
     int n = -1, runs = 0;
+    // tensor memory: two accumulators, two chunks of the rows' scales, all of the weights'
+    const unsigned sfa = tmem + 2 * t.NT, sfb = sfa + 2 * CHUNK_COLUMNS;
 
     if (warp == 0) {
         int slot = 0, phase = 0, issued = 0, weights = 0;
-        for (int u = u0; u < u1 && ok; ++u) {
-            if (!live(u)) continue;
-            const int m0 = u % t.MT * TILE_M;
-            const bool fresh = u / t.MT != n;
-            if (fresh) {
-                n = u / t.MT;
-                if (A4 && runs && !(ok = bar_wait(&bars->b_free, (runs - 1) & 1, dead))) break;
-                ++runs;
-                weights = 0;
-            }
-            for (int ks = 0; ks < t.KS; ++ks) {
-                if (A4 && fresh) {
-                    if (lane == 0) {
+        if (elected()) {
+            for (; at.u < u1 && ok; at.next()) {
+                if (!live(at.u)) continue;
+                const int m0 = at.m * TILE_M;
+                const bool fresh = at.n != n;
+                if (fresh) {
+                    n = at.n;
+                    if (A4 && runs && !(ok = bar_wait_one(&bars->b_free, (runs - 1) & 1, dead))) break;
+                    ++runs;
+                    weights = 0;
+                }
+                for (int ks = 0; ks < t.KS; ++ks) {
+                    if (A4 && fresh) {
                         bar_expect(&bars->b_full[ks], t.NT * 128);
                         tma_load(smem + ks * t.NT * 128, &w_map, ks * 128, n * t.NT, &bars->b_full[ks]);
+                        ++weights;
                     }
-                    ++weights;
-                }
-                if (!(ok = bar_wait(&bars->empty[slot], phase ^ 1, dead))) break;
-                if (lane == 0) {
+                    if (!(ok = bar_wait_one(&bars->empty[slot], phase ^ 1, dead))) break;
                     bar_expect(&bars->a_full[slot], STAGE_A);
                     tma_load(smem + t.off_a + slot * STAGE_A, &a_map, ks * 128, m0, &bars->a_full[slot]);
+                    ++issued;
+                    if (++slot == S) slot = 0, phase ^= 1;
                 }
-                ++issued;
-                if (++slot == S) slot = 0, phase ^= 1;
+            }
+            if (!ok) {                                   // copies in flight end before the CTA does
+                const long long start = clock64();
+                for (int i = 0; i < weights; ++i)
+                    while (!bar_try(&bars->b_full[i], (runs - 1) & 1) && clock64() - start < WAIT_CLOCKS) {}
+                for (int i = 0; i < S && i < issued; ++i) {
+                    if (--slot < 0) slot = S - 1, phase ^= 1;
+                    while (!bar_try(&bars->a_full[slot], phase) && clock64() - start < WAIT_CLOCKS) {}
+                }
             }
         }
-        if (!ok) {                                       // copies in flight end before the CTA does
-            const long long start = clock64();
-            for (int i = 0; i < weights; ++i)
-                while (!bar_try(&bars->b_full[i], (runs - 1) & 1) && clock64() - start < WAIT_CLOCKS) {}
-            for (int i = 0; i < S && i < issued; ++i) {
-                if (--slot < 0) slot = S - 1, phase ^= 1;
-                while (!bar_try(&bars->a_full[slot], phase) && clock64() - start < WAIT_CLOCKS) {}
-            }
-        }
+        __syncwarp();
     } else if (warp == 1) {
         const unsigned idesc = (A4 ? 1u << 7 | 1u << 10 : 0u) | (unsigned)(t.NT >> 3) << 17 | 1u << 23 | 1u << 27;
-        int slot = 0, phase = 0, it = 0, j = 0;
-        for (int u = u0; u < u1 && ok; ++u) {
-            if (!live(u)) continue;
-            const bool fresh = u / t.MT != n;
-            if (fresh) {
-                n = u / t.MT;
-                if (runs && lane == 0) commit(&bars->b_free);
-                if (!(ok = bar_wait(&bars->bs_full, runs++ & 1, dead))) break;
-            }
-            const unsigned acc = tmem + (j & 1) * ACC_COLUMNS;
-            if (!(ok = bar_wait(&bars->acc_free[j & 1], ((j >> 1) & 1) ^ 1, dead))) break;
-            for (int ks = 0; ks < t.KS; ++ks, ++it) {
-                if (fresh && !(ok = bar_wait(&bars->b_full[ks], (runs - 1) & 1, dead))) break;
-                if (!(ok = bar_wait(&bars->a_full[slot], phase, dead) && bar_wait(&bars->s_full[slot], phase, dead))) break;
-                tmem_fence_after();
-                if (lane == 0) {
-                    const unsigned a = smem_at(smem + t.off_a + slot * STAGE_A), b = smem_at(smem + ks * t.NT * 128);
-                    const unsigned sfa = smem_at(smem + t.off_sfa + slot * STAGE_SCALES);
-                    const unsigned column = tmem + SCALE_COLUMNS + (it & 1) * 32;
-                    const int groups = min(GROUPS, p.G - ks * GROUPS);
-                    for (int g = 0; g < groups; ++g) {
-                        const unsigned sfb = smem_at(smem + t.off_sfb + (ks * GROUPS + g) * t.sfb_group);
-                        copy_scales(column + 4 * g, scales_desc(sfa + 512 * g));
-                        copy_scales(column + 8 + 8 * g, scales_desc(sfb));
-                        if (t.sfb_group > 512) copy_scales(column + 12 + 8 * g, scales_desc(sfb + 512));
+        const unsigned a0 = desc_low(smem_at(smem + t.off_a)), b0 = desc_low(smem_at(smem)), b_step = t.NT * 8;
+        const unsigned sfb_step = t.sfb_columns;
+        const int KS = t.KS, G = p.G;
+        if (elected()) {
+            int slot = 0, phase = 0, j = 0, chunk = 0;
+            for (; at.u < u1 && ok; at.next()) {
+                if (!live(at.u)) continue;
+                const bool fresh = at.n != n;
+                if (fresh) {
+                    n = at.n;
+                    if (runs) commit(&bars->b_free);
+                    if (!(ok = bar_wait_one(&bars->bs_full, runs++ & 1, dead))) break;
+                }
+                const unsigned acc = tmem + (j & 1) * t.NT;
+                unsigned b = b0, sa = 0, sb = sfb;
+                if (!(ok = bar_wait_one(&bars->acc_free[j & 1], ((j >> 1) & 1) ^ 1, dead))) break;
+                for (int ks = 0; ks < KS; ++ks) {
+                    if (ks * GROUPS % CHUNK == 0) {          // scales of the next eight groups
+                        if (ks) commit(&bars->s_free[chunk++ & 1]);
+                        if (!(ok = bar_wait_one(&bars->s_full[chunk & 1], (chunk >> 1) & 1, dead))) break;
+                        sa = sfa + (chunk & 1) * CHUNK_COLUMNS;
                     }
-                    const unsigned long long da = operand_desc(a), db = operand_desc(b);
-                    const int steps = A4 ? 2 * groups : 4;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (k >= steps) break;
-                        const int g = A4 ? k >> 1 : 0;
-                        const unsigned id = A4 ? 2 * (k & 1) : k;      // which of the column's four scales to begin with
-                        multiply<A4>(acc, da + 2 * k, db + 2 * k, idesc | id << 4 | id << 29, column + 4 * g, column + 8 + 8 * g,
-                                     ks > 0 || k > 0);
+                    if (fresh && !(ok = bar_wait_one(&bars->b_full[ks], (runs - 1) & 1, dead))) break;
+                    if (!(ok = bar_wait_one(&bars->a_full[slot], phase, dead))) break;
+                    tmem_fence_after();
+                    const unsigned a = a0 + slot * (STAGE_A / 16);
+                    // which of a column's four scales to begin with stands in bits 4 and 29 of the descriptor
+                    if (A4) {
+                        multiply<A4>(acc, a, b, idesc, sa, sb, ks);
+                        multiply<A4>(acc, a + 2, b + 2, idesc | 2u << 4 | 2u << 29, sa, sb, 1);
+                        if (ks * GROUPS + 1 < G) {
+                            multiply<A4>(acc, a + 4, b + 4, idesc, sa + 4, sb + sfb_step, 1);
+                            multiply<A4>(acc, a + 6, b + 6, idesc | 2u << 4 | 2u << 29, sa + 4, sb + sfb_step, 1);
+                        }
+                    } else {
+                        multiply<A4>(acc, a, b, idesc, sa, sb, ks);
+                        multiply<A4>(acc, a + 2, b + 2, idesc | 1u << 4 | 1u << 29, sa, sb, 1);
+                        multiply<A4>(acc, a + 4, b + 4, idesc | 2u << 4 | 2u << 29, sa, sb, 1);
+                        multiply<A4>(acc, a + 6, b + 6, idesc | 3u << 4 | 3u << 29, sa, sb, 1);
                     }
                     commit(&bars->empty[slot]);
+                    b += b_step;
+                    sa += 4 * GROUPS;
+                    sb += sfb_step * GROUPS;
+                    if (++slot == S) slot = 0, phase ^= 1;
                 }
-                __syncwarp();
-                if (++slot == S) slot = 0, phase ^= 1;
+                if (ok) {
+                    commit(&bars->acc_full[j & 1]);
+                    commit(&bars->s_free[chunk++ & 1]);
+                }
+                ++j;
             }
-            if (ok && lane == 0) commit(&bars->acc_full[j & 1]);
-            ++j;
-        }
-        // nothing of this CTA's is under way when the tensor memory is given back
-        if (lane == 0) {
+            // nothing of this CTA's is under way when the tensor memory is given back
             commit(&bars->drained);
             const long long start = clock64();
             while (!bar_try(&bars->drained, 0) && clock64() - start < WAIT_CLOCKS) {}
@@ -479,130 +533,187 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
         __syncwarp();
         tmem_fence_before();
     } else if (warp < 6) {
-        const int lt = tid - 64;
-        int slot = 0, phase = 0;
-        int pending = 0, done = 0;                       // stages whose scales are on their way, slot of the first of them
+        // Tensor memory holds the scales of 32 rows in its 32 lanes, four in a word for the blocks of a group; rows 32 c to
+        // 32 c + 31 are in column c, and each of the four sets of lanes that a warp can write has all of it.
+        const int lt = tid - 64, pieces = (p.G + CHUNK - 1) / CHUNK;
+        const unsigned lanes = (unsigned)(warp & 3) << 21;
+        int chunk = 0, place = 0, round = 0;
         auto deliver = [&](unsigned long long *bar) {
-            fence_async();
             __syncwarp();
             if (lane == 0) bar_arrive(bar);
         };
-        auto deliver_scales = [&]() {
-            deliver(&bars->s_full[done]);
-            if (++done == S) done = 0;
-            --pending;
+        auto deliver_tmem = [&](unsigned long long *bar) {
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            tmem_fence_before();
+            deliver(bar);
         };
-        for (int u = u0; u < u1 && ok; ++u) {
-            if (!live(u)) continue;
-            const bool fresh = u / t.MT != n;
-            uint4 w[UNPACKED];
+        for (; at.u < u1 && ok; at.next()) {
+            if (!live(at.u)) continue;
+            const bool fresh = at.n != n;
+            uint4 q[UNPACKED];
             if (fresh) {
-                // the tiles before need their scales before they are done with their weights
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-                while (pending) deliver_scales();
-                n = u / t.MT;
+                n = at.n;
                 if (runs && !(ok = bar_wait(&bars->b_free, (runs - 1) & 1, dead))) break;
+                tmem_fence_after();
                 ++runs;
-                if (!A4) read_weights(p, t, n * t.NT, 0, lt, w);
-                load_weight_scales(p, t, smem, n * t.NT, lt);
-                deliver(&bars->bs_full);
+                if (!A4) read_weights(p, t, n * t.NT, 0, lt, q);
+                // 16 columns at a time: four groups of up to 128 of W's rows, or two of up to 256
+                const int bits = t.sfb_columns == 8 ? 3 : 2;
+                for (int g0 = 0; g0 < p.G; g0 += 16 >> bits) {
+                    unsigned v[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int g = g0 + (i >> bits), c = (i & ((1 << bits) - 1)) * 32 + lane, row = n * t.NT + c;
+                        v[i] = c < t.NT && row < p.N && g < p.G
+                                   ? __ldg(reinterpret_cast<const unsigned *>(p.w_scales) + (int64_t)row * p.G + g) : 0u;
+                    }
+                    tmem_store16(sfb + lanes + (g0 << bits), v);
+                }
+                deliver_tmem(&bars->bs_full);
             }
-            const int m = u % t.MT * TILE_M + lt;
-            const uint8_t *from = p.a_scales + (int64_t)min(m, batch.rows - 1) * p.G * 4;
-            const unsigned bytes = m < batch.rows ? 4 : 0;
-            for (int ks = 0; ks < t.KS; ++ks) {
-                if (!(ok = bar_wait(&bars->empty[slot], phase ^ 1, dead))) break;
-                const unsigned to = smem_at(smem + t.off_sfa + slot * STAGE_SCALES + (lt & 31) * 16 + (lt >> 5) * 4);
+            if (!(ok = bar_wait(&bars->r_full[place], round, dead))) break;
+            const unsigned *rows = reinterpret_cast<const unsigned *>(smem + t.off_scales + place * 512 * p.G) + lane * p.G;
+            for (int piece = 0; piece < pieces; ++piece, ++chunk) {
+                unsigned w[CHUNK_COLUMNS];               // four rows, eight groups
+                if ((p.G & 3) == 0) {
 #pragma unroll
-                for (int g = 0; g < GROUPS; ++g)
-                    if (ks * GROUPS + g < p.G)
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 512 * g),
-                                     "l"(from + 4 * (ks * GROUPS + g)), "r"(bytes) : "memory");
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                if (!A4 && fresh) {                      // a group of weights behind the next one's reads
-                    uint4 next[UNPACKED];
-                    read_weights(p, t, n * t.NT, ks + 1, lt, next);
-                    put_weights(t, smem + ks * t.NT * 128, lt, w);
-                    deliver(&bars->b_full[ks]);
+                    for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int i = 0; i < UNPACKED; ++i) w[i] = next[i];
+                        for (int h = 0; h < 2; ++h) {
+                            uint4 v = make_uint4(0, 0, 0, 0);
+                            if (piece * CHUNK + 4 * h < p.G)
+                                v = *reinterpret_cast<const uint4 *>(rows + 32 * c * p.G + piece * CHUNK + 4 * h);
+                            w[16 * h + c] = v.x;
+                            w[16 * h + 4 + c] = v.y;
+                            w[16 * h + 8 + c] = v.z;
+                            w[16 * h + 12 + c] = v.w;
+                        }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int g = 0; g < CHUNK; ++g)
+                            w[4 * g + c] = piece * CHUNK + g < p.G ? rows[32 * c * p.G + piece * CHUNK + g] : 0u;
                 }
-                if (++pending > SCALE_LAG) {
-                    asm volatile("cp.async.wait_group %0;" ::"n"(SCALE_LAG) : "memory");
-                    deliver_scales();
+                if (!(ok = bar_wait(&bars->s_free[chunk & 1], ((chunk >> 1) & 1) ^ 1, dead))) break;
+                tmem_fence_after();
+                tmem_store32(sfa + lanes + (chunk & 1) * CHUNK_COLUMNS, w);
+                deliver_tmem(&bars->s_full[chunk & 1]);
+                if (!A4 && fresh && piece == 0)
+                    for (int ks = 0; ks < t.KS; ++ks) {
+                        put_weights(t, smem + ks * t.NT * 128, lt, q);
+                        read_weights(p, t, n * t.NT, ks + 1, lt, q);
+                        fence_async();
+                        deliver(&bars->b_full[ks]);
+                    }
+            }
+            if (!ok) break;
+            deliver(&bars->r_free[place]);
+            if (++place == t.ahead) place = 0, round ^= 1;
+        }
+        tmem_fence_before();
+    } else if (warp == 14) {
+        int place = 0, round = 0, fetched = 0;
+        if (elected()) {
+            const int box = p.G & 1 ? 128 : 256;         // words that are fetched at once
+            for (; at.u < u1 && ok; at.next()) {
+                if (!live(at.u)) continue;
+                if (!(ok = bar_wait_one(&bars->r_free[place], round ^ 1, dead))) break;
+                bar_expect(&bars->r_full[place], 512 * p.G);
+                for (int i = 0; i < TILE_M * p.G; i += box)
+                    tma_load1(smem + t.off_scales + place * 512 * p.G + 4 * i, &s_map, at.m * TILE_M * p.G + i, &bars->r_full[place]);
+                ++fetched;
+                if (++place == t.ahead) place = 0, round ^= 1;
+            }
+            if (!ok) {
+                const long long start = clock64();
+                for (int i = 0; i < t.ahead && i < fetched; ++i) {
+                    if (--place < 0) place = t.ahead - 1, round ^= 1;
+                    while (!bar_try(&bars->r_full[place], round) && clock64() - start < WAIT_CLOCKS) {}
                 }
-                if (++slot == S) slot = 0, phase ^= 1;
             }
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        while (pending) deliver_scales();
+        __syncwarp();
     } else {
-        const int q = warp & 3, half = (warp - 6) >> 2;  // the lanes of tensor memory that this warp may read; every other piece
-        char *stage = smem + t.off_out + (warp - 6) * WRITER_BYTES;
+        // Two sets of four warps take tiles in turns, each warp the 32 lanes of tensor memory that it may read.
+        const int q = warp & 3, set = (warp - 6) >> 2;
+        char *const stage = smem + t.off_out + (warp - 6) * WRITER_BYTES;
         float *bias = bars->bias[warp - 6];
         int j = 0;
         const int size = p.bf16_out ? 2 : 4, unit = 16 / size, wide = 128 / size;      // a piece: 32 rows of 128 bytes
-        const bool vec = (p.N & (unit - 1)) == 0 && (reinterpret_cast<uintptr_t>(p.out) & 15) == 0;
-        for (int u = u0; u < u1 && ok; ++u) {
-            const int n0 = u / t.MT * t.NT, row0 = u % t.MT * TILE_M + 32 * q, cols = min(t.NT, p.N - n0);
+        for (; at.u < u1 && ok; at.next()) {
+            const bool alive = live(at.u);
+            if ((alive ? j++ : at.u) & 1 ^ set) continue;
+            const int n0 = at.n * t.NT, row0 = at.m * TILE_M + 32 * q, cols = min(t.NT, p.N - n0);
             const int rows = min(32, batch.rows - row0);     // may be negative
-            const bool alive = live(u), valid = alive && batch.holds(row0 + lane);
-            const bool some = __any_sync(~0u, valid);
-            if (u / t.MT != n) {
-                n = u / t.MT;
+            const bool valid = alive && batch.holds(row0 + lane);
+            const bool some = __any_sync(~0u, valid), all = __all_sync(~0u, valid);
+            if (at.n != n) {
+                n = at.n;
                 __syncwarp();
-                for (int c = lane; c < MAX_NT; c += 32) bias[c] = p.bias && c < cols ? __ldg(p.bias + n0 + c) : 0.f;
+                if (p.bias)
+                    for (int c = lane; c < MAX_NT + 32; c += 32) bias[c] = c < cols ? __ldg(p.bias + n0 + c) : 0.f;
                 __syncwarp();
             }
             char *out = static_cast<char *>(p.out) + ((int64_t)row0 * p.N + n0) * size;
             if (alive) {
-                if (!(ok = bar_wait(&bars->acc_full[j & 1], (j >> 1) & 1, dead))) break;
+                if (!(ok = bar_wait(&bars->acc_full[set], (j - 1) >> 1 & 1, dead))) break;
                 tmem_fence_after();
             }
-            const unsigned acc = tmem + (j & 1) * ACC_COLUMNS + ((unsigned)q << 21);
-            for (int c0 = half * wide; c0 < cols; c0 += 2 * wide) {
+            const unsigned acc = tmem + set * t.NT + ((unsigned)q << 21);
+            for (int c0 = 0; c0 < cols; c0 += wide) {
                 unsigned r[2][32];
                 const bool both = p.bf16_out && c0 + 32 < cols;      // 64 columns of 16 bits, 32 of 32
+                auto add_bias = [&](unsigned *v, int c) {            // two columns at a time
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint4 z = reinterpret_cast<const uint4 *>(bias + c)[i];
+                        add_pair(v[4 * i], v[4 * i + 1], z.x, z.y);
+                        add_pair(v[4 * i + 2], v[4 * i + 3], z.z, z.w);
+                    }
+                };
                 if (some) {
                     tmem_load32(acc + c0, r[0]);
                     if (both) tmem_load32(acc + c0 + 32, r[1]);
                     tmem_loaded(r[0]);
                     if (both) tmem_loaded(r[1]);
-                }
-                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                __syncwarp();                            // the piece before has left
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (h && !both) break;
-                    float v[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = valid ? __uint_as_float(r[h][i]) + bias[c0 + 32 * h + i] : p.pad;
-                    if (p.bf16_out) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            mx::store8(reinterpret_cast<__nv_bfloat16 *>(stage + lane * 128 + (((4 * h + i) ^ (lane & 7)) << 4)),
-                                       v + 8 * i);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            *reinterpret_cast<float4 *>(stage + lane * 128 + ((i ^ (lane & 7)) << 4)) =
-                                make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    if (p.bias) {
+                        add_bias(r[0], c0);
+                        if (both) add_bias(r[1], c0 + 32);
                     }
                 }
-                if (t.by_tma && (c0 + wide <= cols || n0 + cols == p.N)) {
+                if (alive && c0 + wide >= cols) {            // the accumulator has been taken
+                    tmem_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&bars->acc_free[set]);
+                }
+                if (!all) {                                  // rows of the piece that hold nothing
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) r[h][i] = valid ? r[h][i] : __float_as_uint(p.pad);
+                }
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                __syncwarp();                                // the piece before has left
+                if (p.bf16_out) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (h && !both) break;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            *reinterpret_cast<uint4 *>(stage + lane * 128 + (((4 * h + i) ^ (lane & 7)) << 4)) =
+                                make_uint4(pack2(r[h] + 8 * i), pack2(r[h] + 8 * i + 2), pack2(r[h] + 8 * i + 4), pack2(r[h] + 8 * i + 6));
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i ^ (lane & 7)) << 4)) =
+                            make_uint4(r[0][4 * i], r[0][4 * i + 1], r[0][4 * i + 2], r[0][4 * i + 3]);
+                }
+                if (t.by_tma) {                              // (cut off at the output's edges)
                     fence_async();
                     __syncwarp();
                     if (lane == 0 && rows > 0) tma_store(&out_map, n0 + c0, row0, stage);
-                } else if (vec) {
-                    __syncwarp();
-                    const int i = lane & 7, c = c0 + i * unit;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int y = 4 * k + (lane >> 3);
-                        if (y < rows && c < cols)
-                            *reinterpret_cast<uint4 *>(out + ((int64_t)y * p.N + c) * size) =
-                                *reinterpret_cast<const uint4 *>(stage + y * 128 + ((i ^ (y & 7)) << 4));
-                    }
                 } else {
                     __syncwarp();
                     for (int y = 0; y < rows; ++y)
@@ -615,12 +726,6 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                                 *reinterpret_cast<float *>(to) = *reinterpret_cast<const float *>(from);
                         }
                 }
-            }
-            if (alive) {                                 // all of it has been taken
-                tmem_fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(&bars->acc_free[j & 1]);
-                ++j;
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -644,7 +749,10 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, Tile
     if (KS > MAX_KS) return false;
     for (int tiles = (p.N + MAX_NT - 1) / MAX_NT; tiles <= (p.N + 15) / 16; ++tiles) {
         TilePlan t;
-        t.NT = ((p.N + tiles - 1) / tiles + 15) / 16 * 16;
+        // whole pieces of 128 bytes, so that a tile ends with a piece or with the output's rows
+        const int wide = tiles == 1 ? 16 : p.bf16_out ? 64 : 32;
+        t.NT = ((p.N + tiles - 1) / tiles + wide - 1) / wide * wide;
+        if (t.NT > MAX_NT) continue;
         if (t.NT == last) continue;
         last = t.NT;
         t.KS = KS;
@@ -653,14 +761,22 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, Tile
         const int64_t units = (int64_t)MT * ((p.N + t.NT - 1) / t.NT);
         if (units > INT32_MAX / 2) break;
         t.units = (int)units;
-        t.sfb_group = t.NT > 128 ? 1024 : 512;
-        t.off_sfb = KS * t.NT * 128;
-        t.off_a = (t.off_sfb + p.G * t.sfb_group + 1023) & ~1023;
-        const int fixed = WRITERS * WRITER_BYTES + (int)sizeof(TileBars) + 1024;
-        t.stages = std::min(MAX_STAGES, (ctx->smem_per_sm - 1024 - fixed - t.off_a) / (STAGE_A + STAGE_SCALES));
-        if (t.stages < SCALE_LAG + 1) continue;
-        t.off_sfa = t.off_a + t.stages * STAGE_A;
-        t.off_out = t.off_sfa + t.stages * STAGE_SCALES;
+        t.sfb_columns = t.NT > 128 ? 8 : 4;
+        if (2 * t.NT + 2 * CHUNK_COLUMNS + (t.sfb_columns * p.G + 31) / 32 * 32 > TMEM_COLUMNS) continue;
+        t.off_a = KS * t.NT * 128;                       // (a multiple of 1024, as 16 divides NT)
+        const int fixed = WRITERS * WRITER_BYTES + (int)sizeof(TileBars) + 2048;
+        // the rows' scales of four tiles, of two or one where that leaves room for a stage more, or for three at all
+        const int room = ctx->smem_per_sm - 1024 - fixed - t.off_a, scales = 512 * p.G;
+        t.stages = 0;
+        for (int ahead = MAX_AHEAD; ahead >= 1; ahead /= 2) {
+            const int stages = std::min(MAX_STAGES, (room - ahead * scales) / STAGE_A);
+            if (stages <= t.stages || t.stages >= (ahead == 1 ? 3 : 6)) continue;
+            t.stages = stages;
+            t.ahead = ahead;
+        }
+        if (t.stages < 3) continue;
+        t.off_scales = t.off_a + t.stages * STAGE_A;
+        t.off_out = (t.off_scales + t.ahead * scales + 1023) & ~1023;
         t.off_misc = t.off_out + WRITERS * WRITER_BYTES;
         t.smem = t.off_misc + (int)sizeof(TileBars) + 1024;
         // rounds of tiles on the busiest multiprocessor, their columns and what every tile costs besides
@@ -701,9 +817,15 @@ int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const
         return encode(map, type, 2, base, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                       CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
-    CUtensorMap a, w, out;
+    CUtensorMap a, s, w, out;
     const uint64_t a_bytes = (uint64_t)p.G * (A4 ? 64 : 128), w_bytes = (uint64_t)p.G * 64, size = p.bf16_out ? 2 : 4;
     if (!describe(&a, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<uint8_t *>(p.a), a_bytes, batch.rows, a_bytes, 128, TILE_M))
+        return AUG_ECUDA;
+    const cuuint64_t words[1] = {(cuuint64_t)batch.rows * p.G};      // (a map of one dimension has no strides, but wants a pointer)
+    const cuuint32_t word_box[1] = {p.G & 1 ? 128u : 256u}, word_step[1] = {1};
+    if (encode(&s, CU_TENSOR_MAP_DATA_TYPE_UINT32, 1, const_cast<uint8_t *>(p.a_scales), words, words, word_box, word_step,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return AUG_ECUDA;
     w = out = a;                                         // (those that are not used)
     if (A4 && !describe(&w, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<uint8_t *>(p.w), w_bytes, p.N, w_bytes, 128, t.NT))
@@ -711,7 +833,7 @@ int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const
     if (t.by_tma && !describe(&out, p.bf16_out ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.out, p.N,
                               batch.rows, p.N * size, 128 / (int)size, 32))
         return AUG_ECUDA;
-    tile_product_kernel<A4><<<std::min(t.units, ctx->sm_count), TILE_THREADS, t.smem, ctx->stream>>>(a, w, out, p, batch, t,
+    tile_product_kernel<A4><<<std::min(t.units, ctx->sm_count), TILE_THREADS, t.smem, ctx->stream>>>(a, s, w, out, p, batch, t,
                                                                                                      ctx->status);
     AUG_CUDA_OK(cudaGetLastError());
     ctx->launches++;
@@ -736,6 +858,7 @@ extern "C" int feat_mx_product(AugCtx *ctx, const uint8_t *a_codes_dev, int a_ty
     const RowBatch batch(frame_counts_dev, T_max, B);
     const bool a4 = a_type == AUG_ELEM_MX4;
     TilePlan t;
-    if (batch.rows <= FEW_ROWS || !plan_tiles(ctx, batch.rows, p, a4, &t)) return launch_few_rows(ctx, p, batch, a4);
+    if (batch.rows <= FEW_ROWS || !plan_tiles(ctx, batch.rows, p, a4, &t))
+        return a4 ? launch_few_rows<true>(ctx, p, batch) : launch_few_rows<false>(ctx, p, batch);
     return a4 ? launch_tiles<true>(ctx, p, batch, t) : launch_tiles<false>(ctx, p, batch, t);
 }
