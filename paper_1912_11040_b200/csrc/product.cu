@@ -48,7 +48,6 @@ few_rows_kernel(ProductArgs p, RowBatch batch, int P) {
     const int warp = (blockIdx.x * FEW_THREADS + threadIdx.x) >> 5;
     const int n0 = (warp * per_warp + lane / P) * FEW_COLS, blocks = 4 * p.G;
     for (int row0 = blockIdx.y * R; row0 < batch.rows; row0 += gridDim.y * R) {
-        const int rows = min(R, batch.rows - row0);
         float acc[R][FEW_COLS] = {};
         for (int b = part; b < blocks; b += P) {
             uint4 w[FEW_COLS];
@@ -58,6 +57,16 @@ few_rows_kernel(ProductArgs p, RowBatch batch, int P) {
                 const int n = min(n0 + c, p.N - 1);
                 w[c] = __ldg(reinterpret_cast<const uint4 *>(p.w + (int64_t)n * p.G * 64) + b);
                 sw[c] = __ldg(p.w_scales + (int64_t)n * blocks + b);
+            }
+            unsigned as[R];                              // (the last row again beyond it)
+            uint4 a[R][A4 ? 1 : 2];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int row = min(row0 + r, batch.rows - 1);
+                as[r] = p.a_scales[(int64_t)row * blocks + b];
+                const uint4 *from = reinterpret_cast<const uint4 *>(p.a + (int64_t)row * p.G * (A4 ? 64 : 128));
+#pragma unroll
+                for (int h = 0; h < (A4 ? 1 : 2); ++h) a[r][h] = from[(A4 ? 1 : 2) * b + h];
             }
             if constexpr (A4) {
                 uint2 wv[FEW_COLS][4];
@@ -69,9 +78,7 @@ few_rows_kernel(ProductArgs p, RowBatch batch, int P) {
                 }
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    if (r >= rows) break;
-                    const uint4 q = reinterpret_cast<const uint4 *>(p.a + (int64_t)(row0 + r) * p.G * 64)[b];
-                    const unsigned sa = p.a_scales[(int64_t)(row0 + r) * blocks + b], aw[4] = {q.x, q.y, q.z, q.w};
+                    const unsigned sa = as[r], aw[4] = {a[r][0].x, a[r][0].y, a[r][0].z, a[r][0].w};
                     int dot[FEW_COLS] = {};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -93,11 +100,10 @@ few_rows_kernel(ProductArgs p, RowBatch batch, int P) {
                         mx::unpack8_e2m1(i == 0 ? w[c].x : i == 1 ? w[c].y : i == 2 ? w[c].z : w[c].w, wv[c]);
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        if (r >= rows) break;
-                        const uint2 q = reinterpret_cast<const uint2 *>(p.a + (int64_t)(row0 + r) * p.G * 128)[4 * b + i];
+                        const uint4 q = a[r][i >> 1];
                         float av[8];
-                        mx::unpack4_e4m3(q.x, av);
-                        mx::unpack4_e4m3(q.y, av + 4);
+                        mx::unpack4_e4m3(i & 1 ? q.z : q.x, av);
+                        mx::unpack4_e4m3(i & 1 ? q.w : q.y, av + 4);
 #pragma unroll
                         for (int c = 0; c < FEW_COLS; ++c)
 #pragma unroll
@@ -105,12 +111,9 @@ few_rows_kernel(ProductArgs p, RowBatch batch, int P) {
                     }
                 }
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    if (r >= rows) break;
-                    const unsigned sa = p.a_scales[(int64_t)(row0 + r) * blocks + b];
+                for (int r = 0; r < R; ++r)
 #pragma unroll
-                    for (int c = 0; c < FEW_COLS; ++c) acc[r][c] += scaled(dot[r][c], sa, sw[c], 0);
-                }
+                    for (int c = 0; c < FEW_COLS; ++c) acc[r][c] += scaled(dot[r][c], as[r], sw[c], 0);
             }
         }
         for (int o = P >> 1; o; o >>= 1)
@@ -118,23 +121,19 @@ few_rows_kernel(ProductArgs p, RowBatch batch, int P) {
             for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int c = 0; c < FEW_COLS; ++c) acc[r][c] += __shfl_xor_sync(~0u, acc[r][c], o);
-        if (part == 0) {
+        // every lane has all sums of its columns: each writes some of them
+        for (int k = part; k < R * FEW_COLS; k += P) {
+            float v = 0.f;
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                if (r >= rows) break;
-                const bool valid = batch.holds(row0 + r);
-#pragma unroll
-                for (int c = 0; c < FEW_COLS; ++c) {
-                    const int n = n0 + c;
-                    if (n >= p.N) break;
-                    const float v = valid ? acc[r][c] + (p.bias ? __ldg(p.bias + n) : 0.f) : p.pad;
-                    const int64_t at = (int64_t)(row0 + r) * p.N + n;
-                    if (p.bf16_out)
-                        static_cast<__nv_bfloat16 *>(p.out)[at] = __float2bfloat16_rn(v);
-                    else
-                        static_cast<float *>(p.out)[at] = v;
-                }
-            }
+            for (int i = 0; i < R * FEW_COLS; ++i) v = i == k ? acc[i / FEW_COLS][i % FEW_COLS] : v;
+            const int row = row0 + k / FEW_COLS, n = n0 + k % FEW_COLS;
+            if (row >= batch.rows || n >= p.N) continue;
+            v = batch.holds(row) ? v + (p.bias ? __ldg(p.bias + n) : 0.f) : p.pad;
+            const int64_t at = (int64_t)row * p.N + n;
+            if (p.bf16_out)
+                static_cast<__nv_bfloat16 *>(p.out)[at] = __float2bfloat16_rn(v);
+            else
+                static_cast<float *>(p.out)[at] = v;
         }
     }
 }
@@ -178,7 +177,7 @@ int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch) {
 //
 // 4-bit rows multiply in 4 bits (64 of K an instruction, 256 a stage); 8-bit rows multiply in 8 bits (32 and 128), for
 // which warps 2-5 unpack the weights to e4m3, of which e2m1 is a part, and put them into shared memory.
-constexpr int TILE_M = 128, MAX_NT = 224, TILE_THREADS = 480;
+constexpr int TILE_M = 128, MAX_NT = 224, MAX_NT_UNPACKED = 128, TILE_THREADS = 480;
 constexpr int STAGE_A = TILE_M * 128;
 constexpr int TMEM_COLUMNS = 512;
 constexpr int LIVE_UNITS = 4096;         // tiles of a CTA that are checked for rows with values; later ones count as such
@@ -191,7 +190,6 @@ struct TilePlan {
     int sfb_columns;                     // tensor memory's columns for a group's weight scales: a fourth of 128 or 256
     int ahead;                           // tiles whose scales shared memory has room for
     int off_a, off_scales, off_out, off_misc, smem;
-    bool by_tma;                         // the output's rows can be written by TMA: they start on 16-byte boundaries
 };
 
 struct TileBars {
@@ -331,7 +329,7 @@ __device__ __forceinline__ void e2m1_to_e4m3(unsigned c, unsigned &lo, unsigned 
 }
 
 // One group of 128 of K of NT columns of W, unpacked to e4m3: read, and put into shared memory
-constexpr int UNPACKED = MAX_NT * 4 / LOADERS;           // pieces of 16 bytes a thread, four to a column
+constexpr int UNPACKED = MAX_NT_UNPACKED * 4 / LOADERS;  // pieces of 16 bytes a thread, four to a column
 __device__ __forceinline__ void read_weights(const ProductArgs &p, const TilePlan &t, int n0, int g, int lt, uint4 *q) {
 #pragma unroll
     for (int i = 0; i < UNPACKED; ++i) {
@@ -365,7 +363,7 @@ __device__ bool tile_holds(const RowBatch &batch, int m0) {
     return false;
 }
 
-template <bool A4>
+template <bool A4, bool BF16, bool BY_TMA>
 __global__ void __launch_bounds__(TILE_THREADS, 1)
 tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap s_map, const __grid_constant__ CUtensorMap w_map,
                     const __grid_constant__ CUtensorMap out_map, const ProductArgs p, const RowBatch batch, const TilePlan t,
@@ -550,13 +548,16 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
         for (; at.u < u1 && ok; at.next()) {
             if (!live(at.u)) continue;
             const bool fresh = at.n != n;
-            uint4 q[UNPACKED];
+            uint4 q[2][UNPACKED];
             if (fresh) {
                 n = at.n;
                 if (runs && !(ok = bar_wait(&bars->b_free, (runs - 1) & 1, dead))) break;
                 tmem_fence_after();
                 ++runs;
-                if (!A4) read_weights(p, t, n * t.NT, 0, lt, q);
+                if (!A4) {
+                    read_weights(p, t, n * t.NT, 0, lt, q[0]);
+                    read_weights(p, t, n * t.NT, 1, lt, q[1]);
+                }
                 // 16 columns at a time: four groups of up to 128 of W's rows, or two of up to 256
                 const int bits = t.sfb_columns == 8 ? 3 : 2;
                 for (int g0 = 0; g0 < p.G; g0 += 16 >> bits) {
@@ -600,12 +601,15 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                 tmem_store32(sfa + lanes + (chunk & 1) * CHUNK_COLUMNS, w);
                 deliver_tmem(&bars->s_full[chunk & 1]);
                 if (!A4 && fresh && piece == 0)
-                    for (int ks = 0; ks < t.KS; ++ks) {
-                        put_weights(t, smem + ks * t.NT * 128, lt, q);
-                        read_weights(p, t, n * t.NT, ks + 1, lt, q);
-                        fence_async();
-                        deliver(&bars->b_full[ks]);
-                    }
+                    for (int ks = 0; ks < t.KS; ks += 2)     // a group's reads are on their way while the one before is put
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (ks + h >= t.KS) break;
+                            put_weights(t, smem + (ks + h) * t.NT * 128, lt, q[h]);
+                            read_weights(p, t, n * t.NT, ks + h + 2, lt, q[h]);
+                            fence_async();
+                            deliver(&bars->b_full[ks + h]);
+                        }
             }
             if (!ok) break;
             deliver(&bars->r_free[place]);
@@ -640,7 +644,8 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
         char *const stage = smem + t.off_out + (warp - 6) * WRITER_BYTES;
         float *bias = bars->bias[warp - 6];
         int j = 0;
-        const int size = p.bf16_out ? 2 : 4, unit = 16 / size, wide = 128 / size;      // a piece: 32 rows of 128 bytes
+        constexpr int size = BF16 ? 2 : 4, wide = 128 / size;      // a piece: 32 rows of 128 bytes
+        const int odd_base = (int)(reinterpret_cast<uintptr_t>(p.out) >> 1 & 1);
         for (; at.u < u1 && ok; at.next()) {
             const bool alive = live(at.u);
             if ((alive ? j++ : at.u) & 1 ^ set) continue;
@@ -663,7 +668,7 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
             const unsigned acc = tmem + set * t.NT + ((unsigned)q << 21);
             for (int c0 = 0; c0 < cols; c0 += wide) {
                 unsigned r[2][32];
-                const bool both = p.bf16_out && c0 + 32 < cols;      // 64 columns of 16 bits, 32 of 32
+                const bool both = BF16 && c0 + 32 < cols;      // 64 columns of 16 bits, 32 of 32
                 auto add_bias = [&](unsigned *v, int c) {            // two columns at a time
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -695,36 +700,54 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                 }
                 if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                 __syncwarp();                                // the piece before has left
-                if (p.bf16_out) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (h && !both) break;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            *reinterpret_cast<uint4 *>(stage + lane * 128 + (((4 * h + i) ^ (lane & 7)) << 4)) =
-                                make_uint4(pack2(r[h] + 8 * i), pack2(r[h] + 8 * i + 2), pack2(r[h] + 8 * i + 4), pack2(r[h] + 8 * i + 6));
-                    }
-                } else {
+                // the lane's row as 32 words, four of them at a time
+                const auto word = [&](int i) { return BF16 ? pack2(r[i >> 4] + 2 * (i & 15)) : r[0][i]; };
+                if (BY_TMA) {                                // (cut off at the output's edges)
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i ^ (lane & 7)) << 4)) =
-                            make_uint4(r[0][4 * i], r[0][4 * i + 1], r[0][4 * i + 2], r[0][4 * i + 3]);
-                }
-                if (t.by_tma) {                              // (cut off at the output's edges)
+                            make_uint4(word(4 * i), word(4 * i + 1), word(4 * i + 2), word(4 * i + 3));
                     fence_async();
                     __syncwarp();
                     if (lane == 0 && rows > 0) tma_store(&out_map, n0 + c0, row0, stage);
-                } else {
-                    __syncwarp();
-                    for (int y = 0; y < rows; ++y)
-                        for (int c = lane; c < wide && c0 + c < cols; c += 32) {
-                            const char *from = stage + y * 128 + (((c / unit) ^ (y & 7)) << 4) + c % unit * size;
-                            char *to = out + ((int64_t)y * p.N + c0 + c) * size;
-                            if (p.bf16_out)
-                                *reinterpret_cast<unsigned short *>(to) = *reinterpret_cast<const unsigned short *>(from);
-                            else
-                                *reinterpret_cast<float *>(to) = *reinterpret_cast<const float *>(from);
-                        }
+                    continue;
+                }
+                const int some_cols = min(wide, cols - c0);
+                // A row of 16-bit values that starts between two words of memory: shifted by one, so that its words are those of
+                // memory; the values at its ends are written by themselves.
+                const bool odd = odd_base ^ (p.N & lane & 1) && BF16;
+                const unsigned short first = (unsigned short)word(0), last = (unsigned short)(word(31) >> 16);
+                unsigned before = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    unsigned w[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const unsigned v = word(4 * i + k);
+                        w[k] = odd ? __funnelshift_l(before, v, 16) : v;
+                        before = v;
+                    }
+                    *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+                __syncwarp();
+                char *to = out + (int64_t)c0 * size;
+                const int64_t stride = (int64_t)p.N * size;
+                if (BF16 && lane < rows) {             // ends of this lane's row
+                    unsigned short *mine = reinterpret_cast<unsigned short *>(to + lane * stride);
+                    if (odd) mine[0] = first;
+                    if ((some_cols + odd) & 1 && (some_cols > 1 || !odd)) {
+                        const int e = some_cols - 1, h = e + odd;
+                        mine[e] = h == 64 ? last : *reinterpret_cast<unsigned short *>(stage + lane * 128 + ((h >> 3 ^ (lane & 7)) << 4) + (h & 7) * 2);
+                    }
+                }
+                for (int y0 = 0; y0 < rows; y0 += 8) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int y = y0 + i;
+                        const int skew = BF16 ? odd_base ^ (p.N & i & 1) : 0, e = (BF16 ? 2 * lane : lane) - skew;
+                        const unsigned v = *reinterpret_cast<const unsigned *>(stage + y * 128 + ((lane >> 2 ^ i) << 4) + (lane & 3) * 4);
+                        if (y < rows && e >= 0 && e + BF16 < some_cols) *reinterpret_cast<unsigned *>(to + y * stride + e * size) = v;
+                    }
                 }
             }
         }
@@ -752,11 +775,10 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, Tile
         // whole pieces of 128 bytes, so that a tile ends with a piece or with the output's rows
         const int wide = tiles == 1 ? 16 : p.bf16_out ? 64 : 32;
         t.NT = ((p.N + tiles - 1) / tiles + wide - 1) / wide * wide;
-        if (t.NT > MAX_NT) continue;
+        if (t.NT > (a4 ? MAX_NT : MAX_NT_UNPACKED)) continue;
         if (t.NT == last) continue;
         last = t.NT;
         t.KS = KS;
-        t.by_tma = (int64_t)p.N * (p.bf16_out ? 2 : 4) % 16 == 0 && on16(p.out);
         t.MT = MT;
         const int64_t units = (int64_t)MT * ((p.N + t.NT - 1) / t.NT);
         if (units > INT32_MAX / 2) break;
@@ -806,10 +828,10 @@ EncodeTiled encode_tiled() {
     return f;
 }
 
-template <bool A4>
+template <bool A4, bool BF16, bool BY_TMA>
 int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const TilePlan &t) {
     const EncodeTiled encode = encode_tiled();
-    if (!encode || smem_opt_in<tile_product_kernel<A4>>(ctx->device) != AUG_OK) return AUG_ECUDA;
+    if (!encode || smem_opt_in<tile_product_kernel<A4, BF16, BY_TMA>>(ctx->device) != AUG_OK) return AUG_ECUDA;
     auto describe = [&](CUtensorMap *map, CUtensorMapDataType type, void *base, uint64_t width, uint64_t rows, uint64_t bytes,
                         int box_x, int box_y) {
         const cuuint64_t dims[2] = {width, rows}, strides[1] = {bytes};
@@ -818,7 +840,7 @@ int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const
                       CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
     CUtensorMap a, s, w, out;
-    const uint64_t a_bytes = (uint64_t)p.G * (A4 ? 64 : 128), w_bytes = (uint64_t)p.G * 64, size = p.bf16_out ? 2 : 4;
+    const uint64_t a_bytes = (uint64_t)p.G * (A4 ? 64 : 128), w_bytes = (uint64_t)p.G * 64, size = BF16 ? 2 : 4;
     if (!describe(&a, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<uint8_t *>(p.a), a_bytes, batch.rows, a_bytes, 128, TILE_M))
         return AUG_ECUDA;
     const cuuint64_t words[1] = {(cuuint64_t)batch.rows * p.G};      // (a map of one dimension has no strides, but wants a pointer)
@@ -830,14 +852,22 @@ int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const
     w = out = a;                                         // (those that are not used)
     if (A4 && !describe(&w, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<uint8_t *>(p.w), w_bytes, p.N, w_bytes, 128, t.NT))
         return AUG_ECUDA;
-    if (t.by_tma && !describe(&out, p.bf16_out ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.out, p.N,
+    if (BY_TMA && !describe(&out, BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.out, p.N,
                               batch.rows, p.N * size, 128 / (int)size, 32))
         return AUG_ECUDA;
-    tile_product_kernel<A4><<<std::min(t.units, ctx->sm_count), TILE_THREADS, t.smem, ctx->stream>>>(a, s, w, out, p, batch, t,
+    tile_product_kernel<A4, BF16, BY_TMA><<<std::min(t.units, ctx->sm_count), TILE_THREADS, t.smem, ctx->stream>>>(a, s, w, out, p, batch, t,
                                                                                                      ctx->status);
     AUG_CUDA_OK(cudaGetLastError());
     ctx->launches++;
     return AUG_OK;
+}
+
+template <bool A4>
+int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const TilePlan &t) {
+    // rows that start on 16-byte boundaries can be written by TMA
+    const bool by_tma = (int64_t)p.N * (p.bf16_out ? 2 : 4) % 16 == 0 && on16(p.out);
+    if (p.bf16_out) return by_tma ? launch_tiles<A4, true, true>(ctx, p, batch, t) : launch_tiles<A4, true, false>(ctx, p, batch, t);
+    return by_tma ? launch_tiles<A4, false, true>(ctx, p, batch, t) : launch_tiles<A4, false, false>(ctx, p, batch, t);
 }
 
 }  // namespace
