@@ -5,6 +5,7 @@ library's kernels.  There is no CPU fallback: a missing library raises."""
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -219,16 +220,19 @@ def aug_measure_fp32_peak(stream: Optional[int] = None) -> float:
     return float(out.value)
 
 
+@functools.lru_cache(maxsize=None)
 def feat_mx_code_bytes(mx_type: int, D: int) -> int:
     """Bytes of a row of D microscaled codes (ELEM_MX8 or ELEM_MX4)."""
     return _size(lib().feat_mx_code_bytes(int(mx_type), int(D)), "feat_mx_code_bytes")
 
 
+@functools.lru_cache(maxsize=None)
 def feat_mx_scale_bytes(D: int) -> int:
     """Bytes of a row's scales."""
     return _size(lib().feat_mx_scale_bytes(int(D)), "feat_mx_scale_bytes")
 
 
+@functools.lru_cache(maxsize=None)
 def feat_rms_norm_partial_floats(D: int) -> int:
     """Floats that feat_rms_norm_grad needs for its own use."""
     return _size(lib().feat_rms_norm_partial_floats(int(D)), "feat_rms_norm_partial_floats")
@@ -256,9 +260,10 @@ def feat_vtlp_logmel_noalloc(config: AugConfig, power_dev, counts_dev, table_dev
 def _ptr(t) -> Optional[int]:
     if t is None:
         return None
-    if isinstance(t, np.ndarray):
+    try:
+        return t.data_ptr()
+    except AttributeError:              # a numpy array
         return t.ctypes.data
-    return t.data_ptr()
 
 
 def _check(rc: int, what: str):

@@ -188,6 +188,7 @@ struct TilePlan {
     int NT, KS, stages;                  // columns of a tile, stages along K, depth of the ring
     int MT, units;                       // row tiles, tiles
     int sfb_columns;                     // tensor memory's columns for a group's weight scales: a fourth of 128 or 256
+    bool whole;                          // tiles of whole pieces of 128 bytes: they end with a piece or with the output's rows
     int ahead;                           // tiles whose scales shared memory has room for
     int off_a, off_scales, off_out, off_misc, smem;
 };
@@ -763,8 +764,9 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
     }
 }
 
-// Columns of a tile and what shared memory holds; false where K is too long for 16 columns.
-bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, TilePlan *best) {
+// Columns of a tile and what shared memory holds; false where there is no room for as few as that.  `whole`: tiles of whole
+// pieces; others may have any multiple of 16 columns.
+bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool whole, TilePlan *best) {
     const int groups = a4 ? 2 : 1, KS = (p.G + groups - 1) / groups, MT = (rows + TILE_M - 1) / TILE_M;
     double least = 0;
     bool found = false;
@@ -772,9 +774,9 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, Tile
     if (KS > MAX_KS) return false;
     for (int tiles = (p.N + MAX_NT - 1) / MAX_NT; tiles <= (p.N + 15) / 16; ++tiles) {
         TilePlan t;
-        // whole pieces of 128 bytes, so that a tile ends with a piece or with the output's rows
-        const int wide = tiles == 1 ? 16 : p.bf16_out ? 64 : 32;
+        const int wide = tiles == 1 || !whole ? 16 : p.bf16_out ? 64 : 32;
         t.NT = ((p.N + tiles - 1) / tiles + wide - 1) / wide * wide;
+        t.whole = whole;
         if (t.NT > (a4 ? MAX_NT : MAX_NT_UNPACKED)) continue;
         if (t.NT == last) continue;
         last = t.NT;
@@ -865,7 +867,7 @@ int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const
 template <bool A4>
 int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const TilePlan &t) {
     // rows that start on 16-byte boundaries can be written by TMA
-    const bool by_tma = (int64_t)p.N * (p.bf16_out ? 2 : 4) % 16 == 0 && on16(p.out);
+    const bool by_tma = t.whole && (int64_t)p.N * (p.bf16_out ? 2 : 4) % 16 == 0 && on16(p.out);
     if (p.bf16_out) return by_tma ? launch_tiles<A4, true, true>(ctx, p, batch, t) : launch_tiles<A4, true, false>(ctx, p, batch, t);
     return by_tma ? launch_tiles<A4, false, true>(ctx, p, batch, t) : launch_tiles<A4, false, false>(ctx, p, batch, t);
 }
@@ -888,7 +890,7 @@ extern "C" int feat_mx_product(AugCtx *ctx, const uint8_t *a_codes_dev, int a_ty
     const RowBatch batch(frame_counts_dev, T_max, B);
     const bool a4 = a_type == AUG_ELEM_MX4;
     TilePlan t;
-    if (batch.rows <= FEW_ROWS || !plan_tiles(ctx, batch.rows, p, a4, &t))
+    if (batch.rows <= FEW_ROWS || !(plan_tiles(ctx, batch.rows, p, a4, true, &t) || plan_tiles(ctx, batch.rows, p, a4, false, &t)))
         return a4 ? launch_few_rows<true>(ctx, p, batch) : launch_few_rows<false>(ctx, p, batch);
     return a4 ? launch_tiles<true>(ctx, p, batch, t) : launch_tiles<false>(ctx, p, batch, t);
 }

@@ -233,7 +233,7 @@ template <typename T, int TPR, int E, bool VEC, int Y>
 __global__ void __launch_bounds__(RowPart<T, TPR, E, VEC>::THREADS, RowPart<T, TPR, E, VEC>::norm_ctas())
 rms_norm_kernel(const NormArgs a, const RowBatch batch) {
     using P = RowPart<T, TPR, E, VEC>;
-    constexpr bool AHEAD = VEC ? E * sizeof(T) <= 96 : E <= 16;
+    constexpr bool AHEAD = VEC ? E * sizeof(T) <= 96 : E <= 24;
     __shared__ typename P::Scratch red;
     extern __shared__ __align__(16) float sm[];
     const int l = threadIdx.x % TPR, D = a.D, step = gridDim.x * P::ROWS;
@@ -602,11 +602,11 @@ int norm_by_width(int D, F f) {
         if (D <= 4096) return f.template operator()<T, 128, 32, VEC>();
         if (D <= 8192) return f.template operator()<T, 256, 32, VEC>();
     } else {
-        if constexpr (VEC)
-            if (D <= 768) return f.template operator()<T, 32, 24, VEC>();
+        if constexpr (!VEC)
+            if (D <= 640) return f.template operator()<T, 32, 20, VEC>();
+        if (D <= 768) return f.template operator()<T, 32, 24, VEC>();
         if (D <= 1024) return f.template operator()<T, 64, 16, VEC>();
-        if constexpr (VEC)
-            if (D <= 1536) return f.template operator()<T, 64, 24, VEC>();
+        if (D <= 1536) return f.template operator()<T, 64, 24, VEC>();
         if (D <= 2048) return f.template operator()<T, 128, 16, VEC>();
         if (D <= 4096) return f.template operator()<T, 256, 16, VEC>();
         if (D <= 8192) return f.template operator()<T, 512, 16, VEC>();
@@ -633,6 +633,8 @@ int grad_by_width(int D, F f) {
         if (D <= 8192) return f.template operator()<T, 512, 16, VEC>();
     } else {
         if (D <= 512) return f.template operator()<T, 64, 8, VEC>();
+        if constexpr (!VEC)
+            if (D <= 768) return f.template operator()<T, 64, 12, VEC>();
         if (D <= 1024) return f.template operator()<T, 128, 8, VEC>();
         if (D <= 2048) return f.template operator()<T, 256, 8, VEC>();
         if (D <= 4096) return f.template operator()<T, 512, 8, VEC>();
