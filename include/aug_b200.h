@@ -179,7 +179,7 @@ int aug_destroy(AugCtx *ctx);
 /* Synchronises the context's stream and reads the device status word.
  * *utt_host = first utterance a kernel rejected (-1 if none), *reason_host =
  * 1 n_src out of range, 2 order out of range, 3 bad noise stretch, 4 (with utterance 0) a wait inside
- * feat_mx_product ran out after about two seconds and its output is not complete (nothing else
+ * feat_mx_product ran out after about ten seconds and its output is not complete (nothing else
  * can go wrong on the device short of a launch failure).  A rejected utterance gets zero impulse
  * responses / silent output; nothing faults.  The word is cleared by the read. */
 int aug_last_status(AugCtx *ctx, int *utt_host, int *reason_host);
@@ -316,8 +316,8 @@ int aug_bucket_by_length(const int *lengths_host, int B, int batch, int *perm_ho
  * Operators on the rows of a padded batch, of any width D: features, stacks of them, and what a
  * model's first layers make of them.  Shared by all:
  *   - Rows lie one behind the other, [B][T_max][D].  Row t of utterance b holds values where
- *     t < frame_counts[b]; frame_counts_dev may be NULL: all rows do.  The other rows are not read,
- *     and receive pad_value, or zeros where codes or gradients are written.
+ *     t < frame_counts[b]; frame_counts_dev may be NULL: all rows do.  What the other rows hold does not
+ *     matter; they receive pad_value, or zeros where codes or gradients are written.
  *   - Rows are fp32 or bf16 (AugElem) and aligned to their element; 16-byte aligned rows whose width
  *     is a multiple of 8 are read and written with 128-bit accesses and are faster.
  *   - B * T_max <= AUG_MAX_ROWS, else AUG_ECAP.  An output may be the very buffer of an input of the
@@ -356,7 +356,7 @@ int64_t feat_mx_scale_bytes(int D);
  *   y_dev   y_type: AUG_ELEM_F32 or AUG_ELEM_BF16, [B][T_max][D], or microscaled codes, with scales_dev
  *           (NULL otherwise)
  * eps > 0; D <= AUG_MAX_NORM_WIDTH, else AUG_ECAP.  sum_dev may be x_dev or residual_dev, and y_dev may be
- * either (where y_type is in_type and it is not sum_dev). */
+ * either, where y_type is in_type and it is not sum_dev (else AUG_EINVAL). */
 int feat_rms_norm(AugCtx *ctx, const void *x_dev, const void *residual_dev, int in_type,
                   const float *weight_dev, const int *frame_counts_dev, int B, int T_max, int D, float eps,
                   void *sum_dev, void *y_dev, int y_type, uint8_t *scales_dev);

@@ -173,9 +173,9 @@ struct RowBatch {
 };
 
 // Checks that all operators on rows share; AUG_OK with *none set where there is nothing to do.
-inline int check_rows(const AugCtx *ctx, int B, int T_max, int D, bool *none) {
+inline int check_rows(const AugCtx *ctx, const int *counts, int B, int T_max, int D, bool *none) {
     *none = false;
-    if (!ctx || B < 0) return AUG_EINVAL;
+    if (!ctx || B < 0 || (reinterpret_cast<uintptr_t>(counts) & 3)) return AUG_EINVAL;
     if (B > ctx->cfg.max_batch) return AUG_ECAP;
     if (T_max <= 0 || D < 1) return AUG_EINVAL;
     if ((int64_t)B * T_max > AUG_MAX_ROWS) return AUG_ECAP;

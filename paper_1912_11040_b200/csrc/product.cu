@@ -215,8 +215,8 @@ __device__ __forceinline__ bool bar_try(unsigned long long *b, unsigned parity) 
                  : "=r"(ok) : "r"(smem_at(b)), "r"(parity) : "memory");
     return ok;
 }
-constexpr long long WAIT_CLOCKS = 4000000000ll;
-// Waits for a phase, for at most about two seconds; false, in all lanes, once it or another wait of the
+constexpr long long WAIT_CLOCKS = 20000000000ll;
+// Waits for a phase, for at most about ten seconds; false, in all lanes, once it or another wait of the
 // CTA has run out.
 __device__ __noinline__ bool bar_wait_long(unsigned long long *b, unsigned parity, int *dead) {
     const long long t0 = clock64();
@@ -878,7 +878,7 @@ extern "C" int feat_mx_product(AugCtx *ctx, const uint8_t *a_codes_dev, int a_ty
                                const uint8_t *w_codes_dev, const uint8_t *w_scales_dev, const float *bias_dev,
                                const int *frame_counts_dev, int B, int T_max, int K, int N, void *out_dev, int out_type) {
     bool none;
-    const int rc = check_rows(ctx, B, T_max, K, &none);
+    const int rc = check_rows(ctx, frame_counts_dev, B, T_max, K, &none);
     if (rc != AUG_OK || none) return rc;
     if (N < 1 || !is_mx_type(a_type) || !is_row_type(out_type)) return AUG_EINVAL;
     if (!a_codes_dev || !a_scales_dev || !w_codes_dev || !w_scales_dev || !out_dev) return AUG_EINVAL;

@@ -737,12 +737,14 @@ int feat_rms_norm(AugCtx *ctx, const void *x_dev, const void *residual_dev, int 
                   const int *frame_counts_dev, int B, int T_max, int D, float eps, void *sum_dev, void *y_dev, int y_type,
                   uint8_t *scales_dev) {
     bool none;
-    const int rc = check_rows(ctx, B, T_max, D, &none);
+    const int rc = check_rows(ctx, frame_counts_dev, B, T_max, D, &none);
     if (rc != AUG_OK || none) return rc;
     if (!x_dev || !y_dev || !is_row_type(in_type) || !(is_row_type(y_type) || is_mx_type(y_type))) return AUG_EINVAL;
     if (!(eps > 0.f) || !(eps <= FLT_MAX)) return AUG_EINVAL;
     if (is_mx_type(y_type) != (scales_dev != nullptr)) return AUG_EINVAL;
     if (D > MAX_WIDTH) return AUG_ECAP;
+    // an output over an input of another width, or two outputs in one place, would be written while rows are still read
+    if (y_dev == sum_dev || (y_type != in_type && (y_dev == x_dev || y_dev == residual_dev))) return AUG_EINVAL;
     const uintptr_t rows_at = (uintptr_t)x_dev | (uintptr_t)residual_dev | (uintptr_t)sum_dev;
     if (rows_at & (elem_bytes(in_type) - 1) || (uintptr_t)weight_dev & 3) return AUG_EINVAL;
     if (is_mx_type(y_type) ? !on16(y_dev) || !on16(scales_dev) : ((uintptr_t)y_dev & (elem_bytes(y_type) - 1)) != 0)
@@ -764,7 +766,7 @@ int feat_rms_norm_grad(AugCtx *ctx, const void *h_dev, const void *dy_dev, const
                        const float *weight_dev, const int *frame_counts_dev, int B, int T_max, int D, float eps,
                        void *dx_dev, float *dweight_dev, float *partial_dev) {
     bool none;
-    const int rc = check_rows(ctx, B, T_max, D, &none);
+    const int rc = check_rows(ctx, frame_counts_dev, B, T_max, D, &none);
     if (rc != AUG_OK) return rc;
     if (D > MAX_WIDTH) return AUG_ECAP;
     if (!dweight_dev || (uintptr_t)dweight_dev & 3) return AUG_EINVAL;
@@ -784,7 +786,7 @@ int feat_rms_norm_grad(AugCtx *ctx, const void *h_dev, const void *dy_dev, const
 int feat_mx_quantize(AugCtx *ctx, const void *x_dev, int in_type, const int *frame_counts_dev, int B, int T_max, int D,
                      uint8_t *codes_dev, int mx_type, uint8_t *scales_dev) {
     bool none;
-    const int rc = check_rows(ctx, B, T_max, D, &none);
+    const int rc = check_rows(ctx, frame_counts_dev, B, T_max, D, &none);
     if (rc != AUG_OK || none) return rc;
     if (!x_dev || !codes_dev || !scales_dev || !is_row_type(in_type) || !is_mx_type(mx_type)) return AUG_EINVAL;
     if ((uintptr_t)x_dev & (elem_bytes(in_type) - 1) || !on16(codes_dev) || !on16(scales_dev)) return AUG_EINVAL;
@@ -808,7 +810,7 @@ int feat_mx_quantize(AugCtx *ctx, const void *x_dev, int in_type, const int *fra
 int feat_mx_dequantize(AugCtx *ctx, const uint8_t *codes_dev, int mx_type, const uint8_t *scales_dev,
                        const int *frame_counts_dev, int B, int T_max, int D, void *x_dev, int out_type) {
     bool none;
-    const int rc = check_rows(ctx, B, T_max, D, &none);
+    const int rc = check_rows(ctx, frame_counts_dev, B, T_max, D, &none);
     if (rc != AUG_OK || none) return rc;
     if (!x_dev || !codes_dev || !scales_dev || !is_row_type(out_type) || !is_mx_type(mx_type)) return AUG_EINVAL;
     if ((uintptr_t)x_dev & (elem_bytes(out_type) - 1) || !on16(codes_dev) || !on16(scales_dev)) return AUG_EINVAL;

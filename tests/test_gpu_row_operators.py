@@ -368,6 +368,35 @@ def test_product_of_many_tiles(ctx, kind):
     check_product(ctx, 3, 6000, 128, 40, [5000, 0, 6000], kind, F32)
 
 
+@pytest.mark.parametrize("kind", [MX4, MX8])
+@pytest.mark.parametrize("t", [F32, BF16])
+def test_product_of_long_rows_in_narrow_tiles(ctx, kind, t):
+    """So long that shared memory holds fewer columns of weights than are written at once."""
+    check_product(ctx, 2, 150, 4096, 300, [150, 9], kind, t)
+    check_product(ctx, 1, 129, 6000, 77, None, kind, t)
+
+
+@pytest.mark.parametrize("kind", [MX4, MX8])
+def test_product_whose_weights_change_often(ctx, kind):
+    """Few rows, many columns: a multiprocessor loads weights several times."""
+    check_product(ctx, 2, 65, 256, 16384, [65, 64], kind, BF16)
+    check_product(ctx, 1, 257, 40, 12000, None, kind, F32)
+
+
+@pytest.mark.parametrize("kind", [MX4, MX8])
+def test_product_of_mostly_nothing(ctx, kind):
+    """Tiles, columns and multiprocessors without a row that holds values."""
+    check_product(ctx, 64, 128, 200, 1024, [0] * 63 + [5], kind, BF16)
+    check_product(ctx, 64, 100, 200, 520, [0] * 64, kind, F32)
+    check_product(ctx, 64, 100, 520, 77, [0, 100] * 32, kind, BF16)
+
+
+@pytest.mark.parametrize("N", [1, 2, 31, 33, 63, 64, 65, 127, 129, 193, 225])
+@pytest.mark.parametrize("t,shift", [(F32, 0), (F32, 1), (BF16, 0), (BF16, 1)])
+def test_product_ends_of_rows(ctx, N, t, shift):
+    check_product(ctx, 1, 133, 96, N, [131], MX4, t, shift=shift, seed=N)
+
+
 @pytest.mark.parametrize("t", [F32, BF16])
 def test_product_beside_16_byte_boundaries(ctx, t):
     check_product(ctx, 2, 90, 256, 128, [90, 3], MX4, t, shift=1)
@@ -539,7 +568,7 @@ def test_no_utterances_and_refusals(ctx):
     assert norm() == 0 and norm(B=0) == 0 and norm(B=0, x=None, y=None) == 0
     for bad in (dict(x=None), dict(y=None), dict(t=MX8), dict(t=9), dict(yt=7), dict(yt=-1), dict(T=0), dict(D=0), dict(B=-1),
                 dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(yt=MX8),
-                dict(sc=u), dict(yt=MX4, y=u[4:], sc=u), dict(yt=MX4, y=u, sc=u[4:]), dict(x=u[1:]), dict(w=u[2:])):
+                dict(sc=u), dict(yt=BF16), dict(s=x), dict(c=u[1:]), dict(yt=MX4, y=u[4:], sc=u), dict(yt=MX4, y=u, sc=u[4:]), dict(x=u[1:]), dict(w=u[2:])):
         assert norm(**bad) == E, bad
     for cap in (dict(B=65), dict(D=16385), dict(T=(1 << 30) + 1), dict(B=64, T=1 << 25)):
         assert norm(**cap) == C, cap
