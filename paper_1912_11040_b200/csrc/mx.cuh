@@ -139,6 +139,8 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float *v) {
 }
 __device__ __forceinline__ float as_float(float v) { return v; }
 __device__ __forceinline__ float as_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ unsigned bits1(const float *p) { return *reinterpret_cast<const unsigned *>(p); }
+__device__ __forceinline__ unsigned bits1(const __nv_bfloat16 *p) { return *reinterpret_cast<const unsigned short *>(p); }
 template <typename T>
 __device__ __forceinline__ float load1(const T *p) { return as_float(*p); }
 __device__ __forceinline__ void store1(float *p, float v) { *p = v; }

@@ -26,21 +26,21 @@ struct RowPart {
     static constexpr int norm_ctas() {
         return TPR > 256 ? 1 : E <= 4 ? 4 : E <= 8 ? (!VEC ? 3 : sizeof(T) == 4 ? 4 : 5) : VEC && sizeof(T) == 2 && E <= 16 ? 3 : 2;
     }
-    static constexpr int grad_ctas() { return TPR > 256 || E > 16 ? 1 : E <= 4 || (VEC && E <= 8 && TPR <= 32) ? 3 : 2; }
+    static constexpr int grad_ctas() { return TPR > 256 || E > 16 ? 1 : E <= 4 || (VEC && E <= 8 && TPR <= 32) || (!VEC && E == 12 && sizeof(T) == 4) ? 3 : 2; }
     static __device__ __forceinline__ int column(int l, int step) { return (step * TPR + l) * STEP; }
 
     // Values as they were read, so that the next row's can be on their way in few registers.  What lies beyond the row's
     // width is zero from the start, and nothing but a row that holds values is read into the rest.
     struct Raw {
         uint4 q[VEC ? E * sizeof(T) / 16 : 1];
-        T s[VEC ? 1 : E];
+        unsigned s[VEC ? 1 : E];                         // (the bits of one value each)
         __device__ __forceinline__ Raw() {
             if constexpr (VEC) {
 #pragma unroll
                 for (int i = 0; i < E * (int)sizeof(T) / 16; ++i) q[i] = make_uint4(0, 0, 0, 0);
             } else {
 #pragma unroll
-                for (int e = 0; e < E; ++e) s[e] = T(0.f);
+                for (int e = 0; e < E; ++e) s[e] = 0;
             }
         }
         __device__ __forceinline__ void read(const void *base, int64_t at, int l, int D, bool on) {
@@ -54,14 +54,14 @@ struct RowPart {
 #pragma unroll
                         for (int i = 0; i < W; ++i) q[c * W + i] = reinterpret_cast<const uint4 *>(row + col)[i];
                     } else {
-                        s[c] = row[col];
+                        s[c] = mx::bits1(row + col);
                     }
                 }
             }
         }
         __device__ __forceinline__ float value(int e) const {
             if constexpr (!VEC) {
-                return mx::as_float(s[e]);
+                return __uint_as_float(sizeof(T) == 4 ? s[e] : s[e] << 16);
             } else if constexpr (sizeof(T) == 4) {
                 const uint4 &w = q[e >> 2];
                 return __uint_as_float((e & 3) == 0 ? w.x : (e & 3) == 1 ? w.y : (e & 3) == 2 ? w.z : w.w);
@@ -341,7 +341,7 @@ template <typename T, int TPR, int E, bool VEC>
 __global__ void __launch_bounds__(RowPart<T, TPR, E, VEC>::THREADS, RowPart<T, TPR, E, VEC>::grad_ctas())
 rms_norm_grad_kernel(const GradArgs a, const RowBatch batch) {
     using P = RowPart<T, TPR, E, VEC>;
-    constexpr bool AHEAD = E <= 16;
+    constexpr bool AHEAD = VEC ? E <= 16 : E <= 8;
     __shared__ typename P::Scratch red;
     extern __shared__ __align__(16) float sm[];
     const int l = threadIdx.x % TPR, D = a.D, step = gridDim.x * P::ROWS;
