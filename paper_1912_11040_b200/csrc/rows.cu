@@ -24,7 +24,7 @@ struct RowPart {
     static constexpr int STEP = VEC ? 8 : 1, STEPS = E / STEP;       // values that are accessed together
     // CTAs a multiprocessor of the norm and of its gradient, by the registers that they take
     static constexpr int norm_ctas() {
-        return TPR > 256 ? 1 : E <= 4 ? 4 : E <= 8 ? (!VEC ? 3 : sizeof(T) == 4 ? 4 : 5) : VEC && sizeof(T) == 2 && E <= 16 ? 3 : 2;
+        return TPR > 256 ? 1 : E <= 4 ? 4 : E <= 8 ? (!VEC ? 3 : sizeof(T) == 4 ? 4 : 5) : (VEC && E <= 16 && (sizeof(T) == 2 || TPR == 8)) || (!VEC && E <= 12) ? 3 : 2;
     }
     static constexpr int grad_ctas() { return TPR > 256 || E > 16 ? 1 : E <= 4 || (VEC && E <= 8 && TPR <= 32) || (!VEC && E == 12 && sizeof(T) == 4) ? 3 : 2; }
     static __device__ __forceinline__ int column(int l, int step) { return (step * TPR + l) * STEP; }
@@ -403,23 +403,30 @@ rms_norm_grad_kernel(const GradArgs a, const RowBatch batch) {
         next = later;
     }
     float *mine = a.partial + (int64_t)blockIdx.x * D;
-    if constexpr (P::ROWS > 1) __syncthreads();          // the gains make room for the CTA's shares
-    for (int s = 0; s < P::ROWS; ++s) {                  // one row's threads after the other
-        if ((int)threadIdx.x / TPR == s) {
+    // rows that share a warp are added there; then one warp's, or one row's threads after the other
+#pragma unroll
+    for (int o = TPR; o < 32; o <<= 1) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) dw[e] += __shfl_xor_sync(~0u, dw[e], o);
+    }
+    constexpr int UNIT = TPR < 32 ? 32 : TPR, UNITS = P::THREADS / UNIT;
+    if constexpr (UNITS > 1) __syncthreads();            // the gains make room for the CTA's shares
+    for (int s = 0; s < UNITS; ++s) {
+        if ((int)threadIdx.x / UNIT == s && (int)threadIdx.x % UNIT < TPR) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const int col = P::column(l, e / P::STEP) + e % P::STEP;
                 if (col < D) {
-                    if constexpr (P::ROWS > 1)
+                    if constexpr (UNITS > 1)
                         sm[col] = s ? sm[col] + dw[e] : dw[e];
                     else
                         mine[col] = dw[e];
                 }
             }
         }
-        if constexpr (P::ROWS > 1) __syncthreads();
+        if constexpr (UNITS > 1) __syncthreads();
     }
-    if constexpr (P::ROWS > 1)
+    if constexpr (UNITS > 1)
         for (int col = threadIdx.x; col < D; col += P::THREADS) mine[col] = sm[col];
 }
 
@@ -582,9 +589,13 @@ mx_dequantize_kernel(const uint8_t *codes, const uint8_t *scales, T *x, int D, i
 
 // Threads that share a row, by its width: as few as hold it with so many bytes of values a thread that the next row fits
 // into registers beside it, one warp or less where that will do, without a barrier then.
-template <typename T, bool VEC, typename F>
+template <typename T, bool VEC, bool CODES, typename F>
 int norm_by_width(int D, F f) {
     constexpr bool WIDE = VEC && sizeof(T) == 2;         // 32 values in 64 bytes
+    if constexpr (VEC && !CODES) {                       // (a group of codes takes sixteen threads)
+        if (D <= 64) return f.template operator()<T, 8, 8, VEC>();
+        if (D <= 128) return f.template operator()<T, 8, 16, VEC>();
+    }
     if constexpr (VEC) {
         if (D <= 128) return f.template operator()<T, 16, 8, VEC>();
     } else {
@@ -618,6 +629,7 @@ template <typename T, bool VEC, typename F>
 int grad_by_width(int D, F f) {
     constexpr bool WIDE = VEC && sizeof(T) == 2;
     if constexpr (VEC) {
+        if (D <= 64) return f.template operator()<T, 8, 8, VEC>();
         if (D <= 128) return f.template operator()<T, 16, 8, VEC>();
     } else {
         if (D <= 128) return f.template operator()<T, 32, 4, VEC>();
@@ -658,7 +670,7 @@ struct LaunchNorm {
         return cudaGetLastError() == cudaSuccess ? AUG_OK : AUG_ECUDA;
     }
     template <typename T, bool VEC>
-    int by_width() const { return norm_by_width<T, VEC>(a.D, *this); }
+    int by_width() const { return norm_by_width<T, VEC, IS_CODES<Y>>(a.D, *this); }
 };
 
 struct LaunchGrad {
