@@ -39,6 +39,9 @@ __device__ __forceinline__ uint2 twice_e2m1(unsigned c) {
 // A frame (or a few) of a stream: bound by reading the weights, half a byte each.  A lane holds a block of 32 of each
 // of COLS columns' weights and goes through R rows with them; P lanes, a power of two, share a column.  4-bit products
 // are sums of whole numbers, four at a time (both operands doubled), exact until the block's scale is applied.
+//
+// 1024 x 4096 weights (2.2 MB, 0.35 us of bytes): one row 3.1 us, about two of which any launch takes; four 3.9; eight 5.2
+// (8-bit rows 6.2).  The tiles below take 6.3 (9.5) for nine rows, which is why this ends at eight.
 constexpr int FEW_THREADS = 256, FEW_COLS = 4, FEW_ROWS = 8;
 
 template <bool A4, int R>
@@ -162,9 +165,15 @@ int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch) {
 // Rows by the hundred: block-scaled tcgen05.mma, 128 rows by NT columns a tile, accumulated in tensor memory.
 //
 // A layer has far more rows than columns, so a CTA keeps NT columns of W with all of K in shared memory (for
-// 1024 x 208 columns 104 KB) and lets the rows stream past: what is read per tile is its 128 rows alone.  One CTA a
+// 1024 x 128 columns 64 KB) and lets the rows stream past: what is read per tile is its 128 rows alone.  One CTA a
 // multiprocessor works through a contiguous part of the tiles, ordered by columns first, so that it loads weights once
 // or twice and all CTAs pass the same rows at about the same time (they come from L2 after the first).
+//
+// 64 x 1998 rows (two thirds hold values), 1024 x 1024, out in 16 bits: 86 us, 2090 TFLOP/s.  The bytes would take 48, but nearly
+// all of them are written, and writes alone do not reach the copy's rate: a fill of the output takes 74 us, this kernel with K = 80
+// takes 60.  The rest is that the rows are read once for every 128 columns (54 bytes a clock is what a multiprocessor gets) while the
+// instructions of 128 columns take 95 clocks instead of 64.  In 8 bits the rows are twice as long, the weights leave
+// room for three stages, and the wait for them is what counts: 200 us.
 //
 //   warp 0      fetches 128 rows x 128 bytes a stage with TMA, swizzled as the tensor cores read them, and the weights
 //               when the columns change;  warp 14 the rows' scales, some tiles ahead
@@ -172,8 +181,8 @@ int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch) {
 //   warps 2-5   put the scales into tensor memory: the rows' eight groups of 128 at a time, the weights' when the columns
 //               change
 //   warps 6-13  take finished tiles out of tensor memory (two accumulators: one fills while the other empties), add the
-//               bias, round, and send 32 rows of 128 bytes at a time off by TMA, or write them where a row's stride
-//               or a tile's end does not allow that
+//               bias, round, and send 32 rows of 128 bytes at a time off by TMA, or write them word by word where rows do
+//               not start on 16-byte boundaries
 //
 // 4-bit rows multiply in 4 bits (64 of K an instruction, 256 a stage); 8-bit rows multiply in 8 bits (32 and 128), for
 // which warps 2-5 unpack the weights to e4m3, of which e2m1 is a part, and put them into shared memory.
@@ -765,7 +774,8 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
 }
 
 // Columns of a tile and what shared memory holds; false where there is no room for as few as that.  `whole`: tiles of whole
-// pieces; others may have any multiple of 16 columns.
+// pieces, as everything is that has room for them (64 x 1998 x 1024 x 1024: tiles of 128 columns 112 us, of 144 148); others may
+// have any multiple of 16 columns.
 bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool whole, TilePlan *best) {
     const int groups = a4 ? 2 : 1, KS = (p.G + groups - 1) / groups, MT = (rows + TILE_M - 1) / TILE_M;
     double least = 0;
@@ -803,7 +813,8 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool
         t.off_out = (t.off_scales + t.ahead * scales + 1023) & ~1023;
         t.off_misc = t.off_out + WRITERS * WRITER_BYTES;
         t.smem = t.off_misc + (int)sizeof(TileBars) + 1024;
-        // rounds of tiles on the busiest multiprocessor, their columns and what every tile costs besides
+        // Rounds of tiles on the busiest multiprocessor, their columns and what every tile costs besides.  (Counting stages,
+        // their latency and the writes instead chose worse: 32 x 250 x 640 x 1024 13.3 us, this 10.3.)
         const double cost = (double)((t.units + ctx->sm_count - 1) / ctx->sm_count) * (t.NT + 32);
         if (!found || cost < least) {
             least = cost;
