@@ -15,7 +15,8 @@ HALF = {F32: U32, BF16: 2.0 ** -8}                # of the types
 KIND = {MX8: "mx8", MX4: "mx4"}
 # widths: one value, less than a block, blocks and groups and one more or less, every split of a row over threads,
 # with and without 128-bit accesses
-WIDTHS = [1, 3, 8, 31, 32, 33, 40, 100, 128, 129, 136, 257, 264, 513, 640, 1000, 1024, 1031, 1536, 4096, 4100, 16384]
+WIDTHS = [1, 3, 8, 31, 32, 33, 40, 100, 128, 129, 136, 257, 264, 513, 640, 1000, 1024, 1031, 1536, 2050, 4096, 4100, 6000, 10001,
+          16384]
 PAD = -7.0
 
 
