@@ -156,6 +156,21 @@ struct RowPart {
     }
 };
 
+// 1 / sqrt(x) to its last bit but one: a step of Newton's on the approximation (two units), so that values beside a border of
+// 8 bits fall to the side where they belong as often as the other roundings allow.  0 for infinity.
+__device__ __forceinline__ float reciprocal_sqrt(float x) {
+    const float r = rsqrtf(x), e = fmaf(-x * r, r, 1.f);
+    return x <= FLT_MAX ? fmaf(0.5f * r, e, r) : r;
+}
+// Sum of squares in four parts
+template <int E>
+__device__ __forceinline__ float squares(const float *v, float scale) {
+    float s[4] = {};
+#pragma unroll
+    for (int e = 0; e < E; ++e) s[e & 3] = fmaf(v[e] * scale, v[e] * scale, s[e & 3]);
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
 // Gains that are kept in shared memory, padded with zeros to the columns that a row's threads have
 constexpr int GAINS_SHARED = 4096;
 template <int THREADS>
@@ -267,20 +282,14 @@ rms_norm_kernel(const NormArgs a, const RowBatch batch) {
         const bool later = batch.holds(row + 2 * step);
         // threads of rows that share a warp stay together
         if (TPR < 32 || valid) {
-            float ss = 0.f;
-#pragma unroll
-            for (int e = 0; e < E; ++e) ss = fmaf(v[e], v[e], ss);
-            ss = P::sum(ss, 0.f, red, turn).x;
-            float rs = rsqrtf(fmaf(ss, a.inv_D, a.eps));
+            const float ss = P::sum(squares<E>(v, 1.f), 0.f, red, turn).x;
+            float rs = reciprocal_sqrt(fmaf(ss, a.inv_D, a.eps));
             // squares beyond fp32 (or values that are not finite): once more, scaled down
             const bool big = !(ss <= FLT_MAX);
             if (TPR <= 32 ? __any_sync(~0u, big) : big) {
                 constexpr float DOWN = 0x1p-96f;
-                float s2 = 0.f;
-#pragma unroll
-                for (int e = 0; e < E; ++e) s2 = fmaf(v[e] * DOWN, v[e] * DOWN, s2);
-                s2 = P::sum(s2, 0.f, red, turn).x;
-                if (big) rs = rsqrtf(s2 * a.inv_D) * DOWN;
+                const float s2 = P::sum(squares<E>(v, DOWN), 0.f, red, turn).x;
+                if (big) rs = reciprocal_sqrt(s2 * a.inv_D) * DOWN;
             }
             if (a.sum && valid) P::store(static_cast<T *>(a.sum) + at, l, D, v);
 #pragma unroll
@@ -392,7 +401,7 @@ rms_norm_grad_kernel(const GradArgs a, const RowBatch batch) {
                 dot = fmaf(g[e], h[e], dot);
             }
             const float2 both = P::sum(ss, dot, red, turn);
-            const float rs = rsqrtf(fmaf(both.x, a.inv_D, a.eps)), c = rs * rs * (both.y * a.inv_D);
+            const float rs = reciprocal_sqrt(fmaf(both.x, a.inv_D, a.eps)), c = rs * rs * (both.y * a.inv_D);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 dw[e] = fmaf(dy[e], h[e] * rs, dw[e]);
