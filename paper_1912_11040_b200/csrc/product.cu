@@ -186,17 +186,18 @@ int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch) {
 //
 // 4-bit rows multiply in 4 bits (64 of K an instruction, 256 a stage); 8-bit rows multiply in 8 bits (32 and 128), for
 // which warps 2-5 unpack the weights to e4m3, of which e2m1 is a part, and put them into shared memory.
-constexpr int TILE_M = 128, MAX_NT = 224, MAX_NT_UNPACKED = 128, TILE_THREADS = 480;
+// Tiles of 128 columns at most: of 192 they read the rows less often, but leave shared memory for fewer stages (64 x 1998 rows,
+// 1536 columns: K = 1024 129 us either way, K = 640 103 and 119).
+constexpr int TILE_M = 128, MAX_NT = 128, TILE_THREADS = 480;
 constexpr int STAGE_A = TILE_M * 128;
 constexpr int TMEM_COLUMNS = 512;
 constexpr int LIVE_UNITS = 4096;         // tiles of a CTA that are checked for rows with values; later ones count as such
 constexpr int MAX_STAGES = 8, MAX_KS = 64, MAX_AHEAD = 4;
-constexpr int LOADERS = 128, CHUNK = 8, CHUNK_COLUMNS = 32, WRITERS = 8, PIECE = 4096, WRITER_BYTES = PIECE;
+constexpr int LOADERS = 128, CHUNK = 8, CHUNK_COLUMNS = 32, SFB_COLUMNS = 4, WRITERS = 8, PIECE = 4096, WRITER_BYTES = PIECE;
 
 struct TilePlan {
     int NT, KS, stages;                  // columns of a tile, stages along K, depth of the ring
     int MT, units;                       // row tiles, tiles
-    int sfb_columns;                     // tensor memory's columns for a group's weight scales: a fourth of 128 or 256
     bool whole;                          // tiles of whole pieces of 128 bytes: they end with a piece or with the output's rows
     int ahead;                           // tiles whose scales shared memory has room for
     int off_a, off_scales, off_out, off_misc, smem;
@@ -339,7 +340,7 @@ __device__ __forceinline__ void e2m1_to_e4m3(unsigned c, unsigned &lo, unsigned 
 }
 
 // One group of 128 of K of NT columns of W, unpacked to e4m3: read, and put into shared memory
-constexpr int UNPACKED = MAX_NT_UNPACKED * 4 / LOADERS;  // pieces of 16 bytes a thread, four to a column
+constexpr int UNPACKED = MAX_NT * 4 / LOADERS;  // pieces of 16 bytes a thread, four to a column
 __device__ __forceinline__ void read_weights(const ProductArgs &p, const TilePlan &t, int n0, int g, int lt, uint4 *q) {
 #pragma unroll
     for (int i = 0; i < UNPACKED; ++i) {
@@ -482,7 +483,6 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
     } else if (warp == 1) {
         const unsigned idesc = (A4 ? 1u << 7 | 1u << 10 : 0u) | (unsigned)(t.NT >> 3) << 17 | 1u << 23 | 1u << 27;
         const unsigned a0 = desc_low(smem_at(smem + t.off_a)), b0 = desc_low(smem_at(smem)), b_step = t.NT * 8;
-        const unsigned sfb_step = t.sfb_columns;
         const int KS = t.KS, G = p.G;
         if (elected()) {
             int slot = 0, phase = 0, j = 0, chunk = 0;
@@ -512,8 +512,8 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                         multiply<A4>(acc, a, b, idesc, sa, sb, ks);
                         multiply<A4>(acc, a + 2, b + 2, idesc | 2u << 4 | 2u << 29, sa, sb, 1);
                         if (ks * GROUPS + 1 < G) {
-                            multiply<A4>(acc, a + 4, b + 4, idesc, sa + 4, sb + sfb_step, 1);
-                            multiply<A4>(acc, a + 6, b + 6, idesc | 2u << 4 | 2u << 29, sa + 4, sb + sfb_step, 1);
+                            multiply<A4>(acc, a + 4, b + 4, idesc, sa + 4, sb + SFB_COLUMNS, 1);
+                            multiply<A4>(acc, a + 6, b + 6, idesc | 2u << 4 | 2u << 29, sa + 4, sb + SFB_COLUMNS, 1);
                         }
                     } else {
                         multiply<A4>(acc, a, b, idesc, sa, sb, ks);
@@ -524,7 +524,7 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                     commit(&bars->empty[slot]);
                     b += b_step;
                     sa += 4 * GROUPS;
-                    sb += sfb_step * GROUPS;
+                    sb += SFB_COLUMNS * GROUPS;
                     if (++slot == S) slot = 0, phase ^= 1;
                 }
                 if (ok) {
@@ -568,17 +568,15 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                     read_weights(p, t, n * t.NT, 0, lt, q[0]);
                     read_weights(p, t, n * t.NT, 1, lt, q[1]);
                 }
-                // 16 columns at a time: four groups of up to 128 of W's rows, or two of up to 256
-                const int bits = t.sfb_columns == 8 ? 3 : 2;
-                for (int g0 = 0; g0 < p.G; g0 += 16 >> bits) {
+                for (int g0 = 0; g0 < p.G; g0 += 4) {    // 16 columns at a time: four groups
                     unsigned v[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int g = g0 + (i >> bits), c = (i & ((1 << bits) - 1)) * 32 + lane, row = n * t.NT + c;
+                        const int g = g0 + i / SFB_COLUMNS, c = i % SFB_COLUMNS * 32 + lane, row = n * t.NT + c;
                         v[i] = c < t.NT && row < p.N && g < p.G
                                    ? __ldg(reinterpret_cast<const unsigned *>(p.w_scales) + (int64_t)row * p.G + g) : 0u;
                     }
-                    tmem_store16(sfb + lanes + (g0 << bits), v);
+                    tmem_store16(sfb + lanes + g0 * SFB_COLUMNS, v);
                 }
                 deliver_tmem(&bars->bs_full);
             }
@@ -788,7 +786,7 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool
         const int wide = tiles == 1 || !whole ? 16 : p.bf16_out ? 64 : 32;
         t.NT = ((p.N + tiles - 1) / tiles + wide - 1) / wide * wide;
         t.whole = whole;
-        if (t.NT > (a4 ? MAX_NT : MAX_NT_UNPACKED)) continue;
+        if (t.NT > MAX_NT) continue;
         if (t.NT == last) continue;
         last = t.NT;
         t.KS = KS;
@@ -796,8 +794,7 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool
         const int64_t units = (int64_t)MT * ((p.N + t.NT - 1) / t.NT);
         if (units > INT32_MAX / 2) break;
         t.units = (int)units;
-        t.sfb_columns = t.NT > 128 ? 8 : 4;
-        if (2 * t.NT + 2 * CHUNK_COLUMNS + (t.sfb_columns * p.G + 31) / 32 * 32 > TMEM_COLUMNS) continue;
+        if (2 * t.NT + 2 * CHUNK_COLUMNS + (p.G + 3) / 4 * 16 > TMEM_COLUMNS) continue;
         t.off_a = KS * t.NT * 128;                       // (a multiple of 1024, as 16 divides NT)
         const int fixed = WRITERS * WRITER_BYTES + (int)sizeof(TileBars) + 2048;
         // the rows' scales of four tiles, of two or one where that leaves room for a stage more, or for three at all
