@@ -748,13 +748,24 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                         mine[e] = h == 64 ? last : *reinterpret_cast<unsigned short *>(stage + lane * 128 + ((h >> 3 ^ (lane & 7)) << 4) + (h & 7) * 2);
                     }
                 }
+                // this lane's word of even rows and of odd ones
+                char *next[2];
+                bool inside[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int e = BF16 ? 2 * lane - (odd_base ^ (p.N & h & 1)) : lane;
+                    next[h] = to + h * stride + e * size;
+                    inside[h] = e >= 0 && e + BF16 < some_cols;
+                }
                 for (int y0 = 0; y0 < rows; y0 += 8) {
+                    unsigned v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        v[i] = *reinterpret_cast<const unsigned *>(stage + (y0 + i) * 128 + ((lane >> 2 ^ i) << 4) + (lane & 3) * 4);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int y = y0 + i;
-                        const int skew = BF16 ? odd_base ^ (p.N & i & 1) : 0, e = (BF16 ? 2 * lane : lane) - skew;
-                        const unsigned v = *reinterpret_cast<const unsigned *>(stage + y * 128 + ((lane >> 2 ^ i) << 4) + (lane & 3) * 4);
-                        if (y < rows && e >= 0 && e + BF16 < some_cols) *reinterpret_cast<unsigned *>(to + y * stride + e * size) = v;
+                        if (y0 + i < rows && inside[i & 1]) *reinterpret_cast<unsigned *>(next[i & 1]) = v[i];
+                        next[i & 1] += 2 * stride;
                     }
                 }
             }
