@@ -173,7 +173,7 @@ int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch) {
 // all of them are written, and writes alone do not reach the copy's rate: a fill of the output takes 74 us, this kernel with K = 80
 // takes 60.  The rest is that the rows are read once for every 128 columns (54 bytes a clock is what a multiprocessor gets) while the
 // instructions of 128 columns take 95 clocks instead of 64.  In 8 bits the rows are twice as long, the weights leave
-// room for three stages, and the wait for them is what counts: 200 us.
+// room for four stages, and the wait for them is what counts: 167 us.
 //
 //   warp 0      fetches 128 rows x 128 bytes a stage with TMA, swizzled as the tensor cores read them, and the weights
 //               when the columns change;  warp 14 the rows' scales, some tiles ahead
@@ -193,12 +193,25 @@ constexpr int STAGE_A = TILE_M * 128;
 constexpr int TMEM_COLUMNS = 512;
 constexpr int LIVE_UNITS = 4096;         // tiles of a CTA that are checked for rows with values; later ones count as such
 constexpr int MAX_STAGES = 8, MAX_KS = 64, MAX_AHEAD = 4;
-constexpr int LOADERS = 128, CHUNK = 8, CHUNK_COLUMNS = 32, SFB_COLUMNS = 4, WRITERS = 8, PIECE = 4096, WRITER_BYTES = PIECE;
+constexpr int LOADERS = 128, CHUNK = 8, CHUNK_COLUMNS = 32, SFB_COLUMNS = 4, WRITERS = 8;
+
+// What a writing warp sends off at once: 32 rows of 128 bytes.  8-bit rows and their unpacked weights want the shared memory for
+// stages: with pieces of 64 bytes a fourth one fits beside 1024 rows of weights (64 x 1998 rows 167 us, with whole pieces 200;
+// 4-bit rows have six stages, and are not faster with half the piece).
+constexpr bool half_piece(bool a4, bool bf16, bool by_tma) { return !a4 && bf16 && by_tma; }
+template <bool A4, bool BF16, bool BY_TMA>
+struct Piece {
+    static constexpr int SIZE = BF16 ? 2 : 4, ROW = half_piece(A4, BF16, BY_TMA) ? 64 : 128, COLS = ROW / SIZE, BYTES = 32 * ROW;
+    // where part i, 16 bytes, of a row is kept: as TMA swizzles rows of 128 or 64 bytes
+    static __device__ __forceinline__ int at(int row, int i) {
+        return row * ROW + ((ROW == 128 ? i ^ (row & 7) : i ^ (row >> 1 & 3)) << 4);
+    }
+};
 
 struct TilePlan {
     int NT, KS, stages;                  // columns of a tile, stages along K, depth of the ring
     int MT, units;                       // row tiles, tiles
-    bool whole;                          // tiles of whole pieces of 128 bytes: they end with a piece or with the output's rows
+    bool by_tma;                         // the output is written by TMA
     int ahead;                           // tiles whose scales shared memory has room for
     int off_a, off_scales, off_out, off_misc, smem;
 };
@@ -649,10 +662,11 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
     } else {
         // Two sets of four warps take tiles in turns, each warp the 32 lanes of tensor memory that it may read.
         const int q = warp & 3, set = (warp - 6) >> 2;
-        char *const stage = smem + t.off_out + (warp - 6) * WRITER_BYTES;
+        using P = Piece<A4, BF16, BY_TMA>;
+        char *const stage = smem + t.off_out + (warp - 6) * P::BYTES;
         float *bias = bars->bias[warp - 6];
         int j = 0;
-        constexpr int size = BF16 ? 2 : 4, wide = 128 / size;      // a piece: 32 rows of 128 bytes
+        constexpr int size = P::SIZE, wide = P::COLS;
         const int odd_base = (int)(reinterpret_cast<uintptr_t>(p.out) >> 1 & 1);
         for (; at.u < u1 && ok; at.next()) {
             const bool alive = live(at.u);
@@ -676,7 +690,7 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
             const unsigned acc = tmem + set * t.NT + ((unsigned)q << 21);
             for (int c0 = 0; c0 < cols; c0 += wide) {
                 unsigned r[2][32];
-                const bool both = BF16 && c0 + 32 < cols;      // 64 columns of 16 bits, 32 of 32
+                const bool both = wide > 32 && c0 + 32 < cols;
                 auto add_bias = [&](unsigned *v, int c) {            // two columns at a time
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -712,8 +726,8 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                 const auto word = [&](int i) { return BF16 ? pack2(r[i >> 4] + 2 * (i & 15)) : r[0][i]; };
                 if (BY_TMA) {                                // (cut off at the output's edges)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i ^ (lane & 7)) << 4)) =
+                    for (int i = 0; i < P::ROW / 16; ++i)
+                        *reinterpret_cast<uint4 *>(stage + P::at(lane, i)) =
                             make_uint4(word(4 * i), word(4 * i + 1), word(4 * i + 2), word(4 * i + 3));
                     fence_async();
                     __syncwarp();
@@ -735,7 +749,7 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                         w[k] = odd ? __funnelshift_l(before, v, 16) : v;
                         before = v;
                     }
-                    *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    *reinterpret_cast<uint4 *>(stage + P::at(lane, i)) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
                 __syncwarp();
                 char *to = out + (int64_t)c0 * size;
@@ -745,7 +759,7 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                     if (odd) mine[0] = first;
                     if ((some_cols + odd) & 1 && (some_cols > 1 || !odd)) {
                         const int e = some_cols - 1, h = e + odd;
-                        mine[e] = h == 64 ? last : *reinterpret_cast<unsigned short *>(stage + lane * 128 + ((h >> 3 ^ (lane & 7)) << 4) + (h & 7) * 2);
+                        mine[e] = h == 64 ? last : *reinterpret_cast<unsigned short *>(stage + P::at(lane, h >> 3) + (h & 7) * 2);
                     }
                 }
                 // this lane's word of even rows and of odd ones
@@ -761,7 +775,7 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                     unsigned v[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        v[i] = *reinterpret_cast<const unsigned *>(stage + (y0 + i) * 128 + ((lane >> 2 ^ i) << 4) + (lane & 3) * 4);
+                        v[i] = *reinterpret_cast<const unsigned *>(stage + P::at(y0 + i, lane >> 2) + (lane & 3) * 4);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         if (y0 + i < rows && inside[i & 1]) *reinterpret_cast<unsigned *>(next[i & 1]) = v[i];
@@ -786,6 +800,9 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
 // pieces, as everything is that has room for them (64 x 1998 x 1024 x 1024: tiles of 128 columns 112 us, of 144 148); others may
 // have any multiple of 16 columns.
 bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool whole, TilePlan *best) {
+    // rows that start on 16-byte boundaries can be written by TMA
+    const bool by_tma = whole && (int64_t)p.N * (p.bf16_out ? 2 : 4) % 16 == 0 && on16(p.out);
+    const int piece_bytes = half_piece(a4, p.bf16_out, by_tma) ? 2048 : 4096;
     const int groups = a4 ? 2 : 1, KS = (p.G + groups - 1) / groups, MT = (rows + TILE_M - 1) / TILE_M;
     double least = 0;
     bool found = false;
@@ -796,7 +813,7 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool
         TilePlan t;
         const int wide = tiles == 1 || !whole ? 16 : p.bf16_out ? 64 : 32;
         t.NT = ((p.N + tiles - 1) / tiles + wide - 1) / wide * wide;
-        t.whole = whole;
+        t.by_tma = by_tma;
         if (t.NT > MAX_NT) continue;
         if (t.NT == last) continue;
         last = t.NT;
@@ -807,7 +824,7 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool
         t.units = (int)units;
         if (2 * t.NT + 2 * CHUNK_COLUMNS + (p.G + 3) / 4 * 16 > TMEM_COLUMNS) continue;
         t.off_a = KS * t.NT * 128;                       // (a multiple of 1024, as 16 divides NT)
-        const int fixed = WRITERS * WRITER_BYTES + (int)sizeof(TileBars) + 2048;
+        const int fixed = WRITERS * piece_bytes + (int)sizeof(TileBars) + 2048;
         // the rows' scales of four tiles, of two or one where that leaves room for a stage more, or for three at all
         const int room = ctx->smem_per_sm - 1024 - fixed - t.off_a, scales = 512 * p.G;
         t.stages = 0;
@@ -820,7 +837,7 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool
         if (t.stages < 3) continue;
         t.off_scales = t.off_a + t.stages * STAGE_A;
         t.off_out = (t.off_scales + t.ahead * scales + 1023) & ~1023;
-        t.off_misc = t.off_out + WRITERS * WRITER_BYTES;
+        t.off_misc = t.off_out + WRITERS * piece_bytes;
         t.smem = t.off_misc + (int)sizeof(TileBars) + 1024;
         // Rounds of tiles on the busiest multiprocessor, their columns and what every tile costs besides.  (Counting stages,
         // their latency and the writes instead chose worse: 32 x 250 x 640 x 1024 13.3 us, this 10.3.)
@@ -852,13 +869,14 @@ EncodeTiled encode_tiled() {
 
 template <bool A4, bool BF16, bool BY_TMA>
 int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const TilePlan &t) {
+    using P = Piece<A4, BF16, BY_TMA>;
     const EncodeTiled encode = encode_tiled();
     if (!encode || smem_opt_in<tile_product_kernel<A4, BF16, BY_TMA>>(ctx->device) != AUG_OK) return AUG_ECUDA;
     auto describe = [&](CUtensorMap *map, CUtensorMapDataType type, void *base, uint64_t width, uint64_t rows, uint64_t bytes,
-                        int box_x, int box_y) {
+                        int box_x, int box_y, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
         const cuuint64_t dims[2] = {width, rows}, strides[1] = {bytes};
         const cuuint32_t box[2] = {(cuuint32_t)box_x, (cuuint32_t)box_y}, steps[2] = {1, 1};
-        return encode(map, type, 2, base, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+        return encode(map, type, 2, base, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                       CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
     CUtensorMap a, s, w, out;
@@ -875,7 +893,7 @@ int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const
     if (A4 && !describe(&w, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<uint8_t *>(p.w), w_bytes, p.N, w_bytes, 128, t.NT))
         return AUG_ECUDA;
     if (BY_TMA && !describe(&out, BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.out, p.N,
-                              batch.rows, p.N * size, 128 / (int)size, 32))
+                              batch.rows, p.N * size, P::COLS, 32, P::ROW == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
         return AUG_ECUDA;
     tile_product_kernel<A4, BF16, BY_TMA><<<std::min(t.units, ctx->sm_count), TILE_THREADS, t.smem, ctx->stream>>>(a, s, w, out, p, batch, t,
                                                                                                      ctx->status);
@@ -886,10 +904,8 @@ int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const
 
 template <bool A4>
 int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const TilePlan &t) {
-    // rows that start on 16-byte boundaries can be written by TMA
-    const bool by_tma = t.whole && (int64_t)p.N * (p.bf16_out ? 2 : 4) % 16 == 0 && on16(p.out);
-    if (p.bf16_out) return by_tma ? launch_tiles<A4, true, true>(ctx, p, batch, t) : launch_tiles<A4, true, false>(ctx, p, batch, t);
-    return by_tma ? launch_tiles<A4, false, true>(ctx, p, batch, t) : launch_tiles<A4, false, false>(ctx, p, batch, t);
+    if (p.bf16_out) return t.by_tma ? launch_tiles<A4, true, true>(ctx, p, batch, t) : launch_tiles<A4, true, false>(ctx, p, batch, t);
+    return t.by_tma ? launch_tiles<A4, false, true>(ctx, p, batch, t) : launch_tiles<A4, false, false>(ctx, p, batch, t);
 }
 
 }  // namespace
