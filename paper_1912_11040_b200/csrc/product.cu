@@ -169,11 +169,11 @@ int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch) {
 // multiprocessor works through a contiguous part of the tiles, ordered by columns first, so that it loads weights once
 // or twice and all CTAs pass the same rows at about the same time (they come from L2 after the first).
 //
-// 64 x 1998 rows (two thirds hold values), 1024 x 1024, out in 16 bits: 86 us, 2090 TFLOP/s.  The bytes would take 48, but nearly
+// 64 x 1998 rows (two thirds hold values), 1024 x 1024, out in 16 bits: 83 us, 2180 TFLOP/s.  The bytes would take 48, but nearly
 // all of them are written, and writes alone do not reach the copy's rate: a fill of the output takes 74 us, this kernel with K = 80
-// takes 60.  The rest is that the rows are read once for every 128 columns (54 bytes a clock is what a multiprocessor gets) while the
+// takes 58.  The rest is that the rows are read once for every 128 columns (54 bytes a clock is what a multiprocessor gets) while the
 // instructions of 128 columns take 95 clocks instead of 64.  In 8 bits the rows are twice as long, the weights leave
-// room for four stages, and the wait for them is what counts: 167 us.
+// room for four stages, and the wait for them is what counts: 159 us.
 //
 //   warp 0      fetches 128 rows x 128 bytes a stage with TMA, swizzled as the tensor cores read them, and the weights
 //               when the columns change;  warp 14 the rows' scales, some tiles ahead
@@ -181,7 +181,7 @@ int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch) {
 //   warps 2-5   put the scales into tensor memory: the rows' eight groups of 128 at a time, the weights' when the columns
 //               change
 //   warps 6-13  take finished tiles out of tensor memory (two accumulators: one fills while the other empties), add the
-//               bias, round, and send 32 rows of 128 bytes at a time off by TMA, or write them word by word where rows do
+//               bias, round, and send 32 rows of 64 or 128 bytes at a time off by TMA, or write them word by word where rows do
 //               not start on 16-byte boundaries
 //
 // 4-bit rows multiply in 4 bits (64 of K an instruction, 256 a stage); 8-bit rows multiply in 8 bits (32 and 128), for
@@ -195,13 +195,20 @@ constexpr int LIVE_UNITS = 4096;         // tiles of a CTA that are checked for 
 constexpr int MAX_STAGES = 8, MAX_KS = 64, MAX_AHEAD = 4;
 constexpr int LOADERS = 128, CHUNK = 8, CHUNK_COLUMNS = 32, SFB_COLUMNS = 4, WRITERS = 8;
 
-// What a writing warp sends off at once: 32 rows of 128 bytes.  8-bit rows and their unpacked weights want the shared memory for
-// stages: with pieces of 64 bytes a fourth one fits beside 1024 rows of weights (64 x 1998 rows 167 us, with whole pieces 200;
-// 4-bit rows have six stages, and are not faster with half the piece).
-constexpr bool half_piece(bool a4, bool bf16, bool by_tma) { return !a4 && bf16 && by_tma; }
-template <bool A4, bool BF16, bool BY_TMA>
+// How tiles are written, by pieces of 32 rows that a writing warp keeps in shared memory and sends off at once: 128 bytes a row word by
+// word (rows that do not start on 16-byte boundaries), or by TMA 128 bytes a row, or 64.  Half pieces leave room for
+// stages: beside 1024 rows of 8-bit weights a fourth one fits (64 x 1998 rows 159 us, with whole pieces 200); 4-bit rows with
+// K = 640 take 69 and 76 us.  But where they do not start on their own boundaries (1000 columns) 4-bit rows are slower for
+// them, 64 x 998 x 640 70 and 62 us, 8-bit rows still faster, 24 x 798 x 1000 33 and 36.
+enum Out { WORDS, WHOLE, HALF };
+Out how_to_write(const ProductArgs &p, bool a4, bool pieces) {
+    const int64_t row = (int64_t)p.N * (p.bf16_out ? 2 : 4);
+    if (!pieces || row % 16 != 0 || !on16(p.out)) return WORDS;
+    return p.bf16_out && (!a4 || (row % 64 == 0 && (reinterpret_cast<uintptr_t>(p.out) & 63) == 0)) ? HALF : WHOLE;
+}
+template <bool BF16, Out OUT>
 struct Piece {
-    static constexpr int SIZE = BF16 ? 2 : 4, ROW = half_piece(A4, BF16, BY_TMA) ? 64 : 128, COLS = ROW / SIZE, BYTES = 32 * ROW;
+    static constexpr int SIZE = BF16 ? 2 : 4, ROW = OUT == HALF ? 64 : 128, COLS = ROW / SIZE, BYTES = 32 * ROW;
     // where part i, 16 bytes, of a row is kept: as TMA swizzles rows of 128 or 64 bytes
     static __device__ __forceinline__ int at(int row, int i) {
         return row * ROW + ((ROW == 128 ? i ^ (row & 7) : i ^ (row >> 1 & 3)) << 4);
@@ -211,7 +218,7 @@ struct Piece {
 struct TilePlan {
     int NT, KS, stages;                  // columns of a tile, stages along K, depth of the ring
     int MT, units;                       // row tiles, tiles
-    bool by_tma;                         // the output is written by TMA
+    Out out;
     int ahead;                           // tiles whose scales shared memory has room for
     int off_a, off_scales, off_out, off_misc, smem;
 };
@@ -387,7 +394,7 @@ __device__ bool tile_holds(const RowBatch &batch, int m0) {
     return false;
 }
 
-template <bool A4, bool BF16, bool BY_TMA>
+template <bool A4, bool BF16, Out OUT>
 __global__ void __launch_bounds__(TILE_THREADS, 1)
 tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap s_map, const __grid_constant__ CUtensorMap w_map,
                     const __grid_constant__ CUtensorMap out_map, const ProductArgs p, const RowBatch batch, const TilePlan t,
@@ -662,7 +669,7 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
     } else {
         // Two sets of four warps take tiles in turns, each warp the 32 lanes of tensor memory that it may read.
         const int q = warp & 3, set = (warp - 6) >> 2;
-        using P = Piece<A4, BF16, BY_TMA>;
+        using P = Piece<BF16, OUT>;
         char *const stage = smem + t.off_out + (warp - 6) * P::BYTES;
         float *bias = bars->bias[warp - 6];
         int j = 0;
@@ -724,7 +731,7 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                 __syncwarp();                                // the piece before has left
                 // the lane's row as 32 words, four of them at a time
                 const auto word = [&](int i) { return BF16 ? pack2(r[i >> 4] + 2 * (i & 15)) : r[0][i]; };
-                if (BY_TMA) {                                // (cut off at the output's edges)
+                if (OUT != WORDS) {                                // (cut off at the output's edges)
 #pragma unroll
                     for (int i = 0; i < P::ROW / 16; ++i)
                         *reinterpret_cast<uint4 *>(stage + P::at(lane, i)) =
@@ -800,9 +807,8 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
 // pieces, as everything is that has room for them (64 x 1998 x 1024 x 1024: tiles of 128 columns 112 us, of 144 148); others may
 // have any multiple of 16 columns.
 bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool whole, TilePlan *best) {
-    // rows that start on 16-byte boundaries can be written by TMA
-    const bool by_tma = whole && (int64_t)p.N * (p.bf16_out ? 2 : 4) % 16 == 0 && on16(p.out);
-    const int piece_bytes = half_piece(a4, p.bf16_out, by_tma) ? 2048 : 4096;
+    const Out out = how_to_write(p, a4, whole);
+    const int piece_bytes = 32 * (out == HALF ? 64 : 128);
     const int groups = a4 ? 2 : 1, KS = (p.G + groups - 1) / groups, MT = (rows + TILE_M - 1) / TILE_M;
     double least = 0;
     bool found = false;
@@ -813,7 +819,7 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool
         TilePlan t;
         const int wide = tiles == 1 || !whole ? 16 : p.bf16_out ? 64 : 32;
         t.NT = ((p.N + tiles - 1) / tiles + wide - 1) / wide * wide;
-        t.by_tma = by_tma;
+        t.out = out;
         if (t.NT > MAX_NT) continue;
         if (t.NT == last) continue;
         last = t.NT;
@@ -867,11 +873,11 @@ EncodeTiled encode_tiled() {
     return f;
 }
 
-template <bool A4, bool BF16, bool BY_TMA>
+template <bool A4, bool BF16, Out OUT>
 int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const TilePlan &t) {
-    using P = Piece<A4, BF16, BY_TMA>;
+    using P = Piece<BF16, OUT>;
     const EncodeTiled encode = encode_tiled();
-    if (!encode || smem_opt_in<tile_product_kernel<A4, BF16, BY_TMA>>(ctx->device) != AUG_OK) return AUG_ECUDA;
+    if (!encode || smem_opt_in<tile_product_kernel<A4, BF16, OUT>>(ctx->device) != AUG_OK) return AUG_ECUDA;
     auto describe = [&](CUtensorMap *map, CUtensorMapDataType type, void *base, uint64_t width, uint64_t rows, uint64_t bytes,
                         int box_x, int box_y, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
         const cuuint64_t dims[2] = {width, rows}, strides[1] = {bytes};
@@ -892,10 +898,10 @@ int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const
     w = out = a;                                         // (those that are not used)
     if (A4 && !describe(&w, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<uint8_t *>(p.w), w_bytes, p.N, w_bytes, 128, t.NT))
         return AUG_ECUDA;
-    if (BY_TMA && !describe(&out, BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.out, p.N,
+    if (OUT != WORDS && !describe(&out, BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.out, p.N,
                               batch.rows, p.N * size, P::COLS, 32, P::ROW == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
         return AUG_ECUDA;
-    tile_product_kernel<A4, BF16, BY_TMA><<<std::min(t.units, ctx->sm_count), TILE_THREADS, t.smem, ctx->stream>>>(a, s, w, out, p, batch, t,
+    tile_product_kernel<A4, BF16, OUT><<<std::min(t.units, ctx->sm_count), TILE_THREADS, t.smem, ctx->stream>>>(a, s, w, out, p, batch, t,
                                                                                                      ctx->status);
     AUG_CUDA_OK(cudaGetLastError());
     ctx->launches++;
@@ -904,8 +910,10 @@ int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const
 
 template <bool A4>
 int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const TilePlan &t) {
-    if (p.bf16_out) return t.by_tma ? launch_tiles<A4, true, true>(ctx, p, batch, t) : launch_tiles<A4, true, false>(ctx, p, batch, t);
-    return t.by_tma ? launch_tiles<A4, false, true>(ctx, p, batch, t) : launch_tiles<A4, false, false>(ctx, p, batch, t);
+    if (!p.bf16_out) return t.out == WORDS ? launch_tiles<A4, false, WORDS>(ctx, p, batch, t) : launch_tiles<A4, false, WHOLE>(ctx, p, batch, t);
+    if constexpr (A4)
+        if (t.out == WHOLE) return launch_tiles<A4, true, WHOLE>(ctx, p, batch, t);
+    return t.out == WORDS ? launch_tiles<A4, true, WORDS>(ctx, p, batch, t) : launch_tiles<A4, true, HALF>(ctx, p, batch, t);
 }
 
 }  // namespace

@@ -403,6 +403,13 @@ def test_product_beside_16_byte_boundaries(ctx, t):
     check_product(ctx, 2, 90, 256, 128, [90, 3], MX4, t, shift=1)
 
 
+@pytest.mark.parametrize("kind", [MX4, MX8])
+@pytest.mark.parametrize("shift", [8, 16, 32])
+def test_product_between_64_byte_boundaries(ctx, kind, shift):
+    check_product(ctx, 2, 190, 256, 320, [190, 3], kind, BF16, shift=shift)
+    check_product(ctx, 2, 190, 256, 328, [190, 3], kind, F32, shift=shift // 2)
+
+
 @pytest.mark.parametrize("rows_", [1, 130])
 @pytest.mark.parametrize("kind", [MX4, MX8])
 def test_product_of_a_block_that_is_not_finite(ctx, rows_, kind):
