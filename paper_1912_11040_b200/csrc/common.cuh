@@ -130,7 +130,7 @@ inline int smem_opt_in(int device) {
     return AUG_OK;
 }
 
-// Kernels of aug_pipeline follow one another without the gap of a full launch: a chained kernel may
+// Kernels of aug_pipeline, and those on rows, follow one another without the gap of a full launch: a chained kernel may
 // start while the one before it on the stream is still running, as soon as all CTAs of that one
 // have called chain_next() or ended (they call it towards their end: CTAs that arrive early and
 // wait take room and slowed long kernels down, 1083 -> 1189 us on 128 x 8 s with 24000 taps); it calls

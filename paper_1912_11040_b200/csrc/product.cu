@@ -41,7 +41,7 @@ __device__ __forceinline__ uint2 twice_e2m1(unsigned c) {
 // are sums of whole numbers, four at a time (both operands doubled), exact until the block's scale is applied.
 //
 // 1024 x 4096 weights (2.2 MB, 0.35 us of bytes): one row 3.1 us, about two of which any launch takes; four 3.9; eight 5.2
-// (8-bit rows 6.2).  The tiles below take 6.3 (9.5) for nine rows, which is why this ends at eight.
+// (8-bit rows 6.2).  The tiles below take 5.8 (9) for nine rows, which is why this ends at eight.
 constexpr int FEW_THREADS = 256, FEW_COLS = 4, FEW_ROWS = 8;
 
 template <bool A4, int R>
@@ -50,6 +50,7 @@ few_rows_kernel(ProductArgs p, RowBatch batch, int P) {
     const int lane = threadIdx.x & 31, part = lane & (P - 1), per_warp = 32 / P;
     const int warp = (blockIdx.x * FEW_THREADS + threadIdx.x) >> 5;
     const int n0 = (warp * per_warp + lane / P) * FEW_COLS, blocks = 4 * p.G;
+    chain_wait();
     for (int row0 = blockIdx.y * R; row0 < batch.rows; row0 += gridDim.y * R) {
         float acc[R][FEW_COLS] = {};
         for (int b = part; b < blocks; b += P) {
@@ -58,8 +59,8 @@ few_rows_kernel(ProductArgs p, RowBatch batch, int P) {
 #pragma unroll
             for (int c = 0; c < FEW_COLS; ++c) {
                 const int n = min(n0 + c, p.N - 1);
-                w[c] = __ldg(reinterpret_cast<const uint4 *>(p.w + (int64_t)n * p.G * 64) + b);
-                sw[c] = __ldg(p.w_scales + (int64_t)n * blocks + b);
+                w[c] = reinterpret_cast<const uint4 *>(p.w + (int64_t)n * p.G * 64)[b];
+                sw[c] = p.w_scales[(int64_t)n * blocks + b];
             }
             unsigned as[R];                              // (the last row again beyond it)
             uint4 a[R][A4 ? 1 : 2];
@@ -131,7 +132,7 @@ few_rows_kernel(ProductArgs p, RowBatch batch, int P) {
             for (int i = 0; i < R * FEW_COLS; ++i) v = i == k ? acc[i / FEW_COLS][i % FEW_COLS] : v;
             const int row = row0 + k / FEW_COLS, n = n0 + k % FEW_COLS;
             if (row >= batch.rows || n >= p.N) continue;
-            v = batch.holds(row) ? v + (p.bias ? __ldg(p.bias + n) : 0.f) : p.pad;
+            v = batch.holds(row) ? v + (p.bias ? p.bias[n] : 0.f) : p.pad;
             const int64_t at = (int64_t)row * p.N + n;
             if (p.bf16_out)
                 static_cast<__nv_bfloat16 *>(p.out)[at] = __float2bfloat16_rn(v);
@@ -148,15 +149,12 @@ int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch) {
     const int cols = FEW_THREADS / P * FEW_COLS;                  // of a CTA
     auto go = [&](auto kern, int R) {
         const dim3 grid((p.N + cols - 1) / cols, std::min((batch.rows + R - 1) / R, 65535));
-        kern<<<grid, FEW_THREADS, 0, ctx->stream>>>(p, batch, P);
+        return launch_chained(kern, grid, FEW_THREADS, 0, ctx->stream, p, batch, P);
     };
-    if (batch.rows == 1)
-        go(few_rows_kernel<A4, 1>, 1);
-    else if (batch.rows <= 4)
-        go(few_rows_kernel<A4, 4>, 4);
-    else
-        go(few_rows_kernel<A4, FEW_ROWS>, FEW_ROWS);
-    AUG_CUDA_OK(cudaGetLastError());
+    const int rc = batch.rows == 1   ? go(few_rows_kernel<A4, 1>, 1)
+                   : batch.rows <= 4 ? go(few_rows_kernel<A4, 4>, 4)
+                                     : go(few_rows_kernel<A4, FEW_ROWS>, FEW_ROWS);
+    if (rc != AUG_OK) return rc;
     ctx->launches++;
     return AUG_OK;
 }
@@ -169,7 +167,7 @@ int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch) {
 // multiprocessor works through a contiguous part of the tiles, ordered by columns first, so that it loads weights once
 // or twice and all CTAs pass the same rows at about the same time (they come from L2 after the first).
 //
-// 64 x 1998 rows (two thirds hold values), 1024 x 1024, out in 16 bits: 83 us, 2180 TFLOP/s.  The bytes would take 48, but nearly
+// 64 x 1998 rows (two thirds hold values), 1024 x 1024, out in 16 bits: 84 us, 2150 TFLOP/s.  The bytes would take 48, but nearly
 // all of them are written, and writes alone do not reach the copy's rate: a fill of the output takes 74 us, this kernel with K = 80
 // takes 58.  The rest is that the rows are read once for every 128 columns (54 bytes a clock is what a multiprocessor gets) while the
 // instructions of 128 columns take 95 clocks instead of 64.  In 8 bits the rows are twice as long, the weights leave
@@ -365,7 +363,7 @@ __device__ __forceinline__ void read_weights(const ProductArgs &p, const TilePla
 #pragma unroll
     for (int i = 0; i < UNPACKED; ++i) {
         const int r = (lt + LOADERS * i) >> 2, n = n0 + r;
-        q[i] = r < t.NT && n < p.N && g < p.G ? __ldg(reinterpret_cast<const uint4 *>(p.w + ((int64_t)n * p.G + g) * 64) + (lt & 3))
+        q[i] = r < t.NT && n < p.N && g < p.G ? reinterpret_cast<const uint4 *>(p.w + ((int64_t)n * p.G + g) * 64)[lt & 3]
                                               : make_uint4(0, 0, 0, 0);
     }
 }
@@ -432,6 +430,7 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                      "r"(TMEM_COLUMNS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    chain_wait();                                        // nothing of memory has been touched so far
     // which tiles have rows with values, a bit each, the same for every role
     for (int w = warp; w < LIVE_UNITS / 32 && 32 * w < u1 - u0; w += TILE_THREADS / 32) {
         const int u = u0 + 32 * w + lane;
@@ -594,7 +593,7 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                     for (int i = 0; i < 16; ++i) {
                         const int g = g0 + i / SFB_COLUMNS, c = i % SFB_COLUMNS * 32 + lane, row = n * t.NT + c;
                         v[i] = c < t.NT && row < p.N && g < p.G
-                                   ? __ldg(reinterpret_cast<const unsigned *>(p.w_scales) + (int64_t)row * p.G + g) : 0u;
+                                   ? reinterpret_cast<const unsigned *>(p.w_scales)[(int64_t)row * p.G + g] : 0u;
                     }
                     tmem_store16(sfb + lanes + g0 * SFB_COLUMNS, v);
                 }
@@ -686,7 +685,7 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
                 n = at.n;
                 __syncwarp();
                 if (p.bias)
-                    for (int c = lane; c < MAX_NT + 32; c += 32) bias[c] = c < cols ? __ldg(p.bias + n0 + c) : 0.f;
+                    for (int c = lane; c < MAX_NT + 32; c += 32) bias[c] = c < cols ? p.bias[n0 + c] : 0.f;
                 __syncwarp();
             }
             char *out = static_cast<char *>(p.out) + ((int64_t)row0 * p.N + n0) * size;
@@ -901,9 +900,9 @@ int launch_tiles(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch, const
     if (OUT != WORDS && !describe(&out, BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.out, p.N,
                               batch.rows, p.N * size, P::COLS, 32, P::ROW == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
         return AUG_ECUDA;
-    tile_product_kernel<A4, BF16, OUT><<<std::min(t.units, ctx->sm_count), TILE_THREADS, t.smem, ctx->stream>>>(a, s, w, out, p, batch, t,
-                                                                                                     ctx->status);
-    AUG_CUDA_OK(cudaGetLastError());
+    if (launch_chained(tile_product_kernel<A4, BF16, OUT>, dim3(std::min(t.units, ctx->sm_count)), TILE_THREADS, t.smem, ctx->stream, a, s, w,
+                       out, p, batch, t, ctx->status) != AUG_OK)
+        return AUG_ECUDA;
     ctx->launches++;
     return AUG_OK;
 }

@@ -540,6 +540,51 @@ def test_captured_replayed_and_on_another_stream(T):
     del g
 
 
+def test_operators_back_to_back_wait_for_one_another():
+    """Every kernel here writes what the next one reads, over what the one before it has read: the same bits as with a
+    wait for the device after every call."""
+    import torch
+    with torch.cuda.stream(torch.cuda.Stream()):
+        back_to_back(context(torch.cuda.current_stream().cuda_stream))
+
+
+def back_to_back(ctx):
+    import torch
+    B, T, D, N = 16, 500, 264, 264
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    w = layer_weights(ctx, D, N, gen)
+    counts = to_counts([T, 3, 0, 499] * 4)
+    first = torch.randn(B, T, D, device="cuda", generator=gen)
+    gain, dw = w["gain"].clone(), torch.empty(D, device="cuda")
+    partial = torch.empty(binding.feat_rms_norm_partial_floats(D), device="cuda")
+    codes = torch.empty(B, T, binding.feat_mx_code_bytes(MX8, D), dtype=torch.uint8, device="cuda")
+    scales = torch.empty(B, T, binding.feat_mx_scale_bytes(D), dtype=torch.uint8, device="cuda")
+
+    def passes(after):
+        x, y = first.clone(), torch.empty(B, T, N, device="cuda")
+        gain.copy_(w["gain"])
+        for _ in range(6):
+            ctx.feat_rms_norm(x, None, F32, gain, counts, B, T, D, EPS, None, codes, MX8, scales)
+            after()
+            ctx.feat_mx_product(codes, MX8, scales, w["codes"], w["scales"], gain, counts, B, T, D, N, y, F32)
+            after()
+            ctx.feat_rms_norm_grad(x, y, None, F32, gain, counts, B, T, D, EPS, x, dw, partial)
+            after()
+            ctx.feat_rms_norm(dw, None, F32, None, None, 1, 1, D, EPS, None, gain, F32, None)
+            after()
+            ctx.feat_mx_quantize(x, F32, counts, B, T, D, codes, MX8, scales)
+            after()
+            ctx.feat_mx_dequantize(codes, MX8, scales, counts, B, T, D, x, F32)
+            after()
+        torch.cuda.synchronize()
+        return host(x), host(y), host(gain)
+
+    want = passes(torch.cuda.synchronize)
+    for _ in range(5):
+        for a, b in zip(passes(lambda: None), want):
+            assert np.array_equal(a, b)
+
+
 def test_two_contexts_at_once():
     """Two streams, the same operators, nothing shared but the weights."""
     import torch

@@ -1,4 +1,7 @@
 """Host side of the operators on rows, and pins of their 64-bit reference, without a GPU."""
+import os
+import re
+
 import numpy as np
 import pytest
 
@@ -60,3 +63,19 @@ def test_reference_gradient_is_that_of_differences():
             up[i] += 1e-5
             down[i] -= 1e-5
             assert (of(up) - of(down)) / 2e-5 == pytest.approx(got[i], abs=1e-8)
+
+
+@pytest.mark.parametrize("name", ["rows.cu", "product.cu"])
+def test_chained_kernels_wait_and_read_coherently(name):
+    """Every kernel is launched behind one that may still be writing, so each waits for it, reads nothing through the
+    non-coherent path, and lets nothing start early but the gradient's own second kernel."""
+    at = os.path.join(os.path.dirname(binding.__file__), "csrc", name)
+    text = re.sub(r"//[^\n]*|/\*.*?\*/", "", open(at).read(), flags=re.S)
+    for word in ("__ldg", "__restrict__", "ld.global.nc", "<<<"):
+        assert word not in text, word
+    kernels = text.split("__global__")[1:]
+    for k in kernels:
+        body = k.split("\n}\n")[0]
+        name = re.search(r"(\w+)\((?:const )?(?:__grid|Norm|Grad|float|T |uint8_t|Product)", body).group(1)
+        assert body.count("chain_wait();") == 1, name
+        assert body.count("chain_next();") == (name == "rms_norm_grad_kernel"), name
