@@ -585,6 +585,50 @@ def back_to_back(ctx):
             assert np.array_equal(a, b)
 
 
+@pytest.mark.parametrize("captured", [False, True])
+def test_operators_after_two_streams_join(captured):
+    """The rows are quantised on one stream, the weights on another; the product waits for both, again and again over
+    the same buffers."""
+    import torch
+    B, T, D, N = 8, 400, 512, 512
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x, w = torch.randn(B, T, D, device="cuda", generator=gen), torch.randn(N, D, device="cuda", generator=gen)
+    bytes_, sbytes = binding.feat_mx_code_bytes(MX4, D), binding.feat_mx_scale_bytes(D)
+    new = lambda *shape: torch.empty(*shape, dtype=torch.uint8, device="cuda")
+    a, sa, q, sq = new(B * T, bytes_), new(B * T, sbytes), new(N, bytes_), new(N, sbytes)
+    y = torch.empty(B, T, N, device="cuda")
+    s, side = torch.cuda.Stream(), torch.cuda.Stream()
+    ctx, beside = context(s.cuda_stream), context(side.cuda_stream)
+
+    def step():
+        side.wait_stream(s)
+        beside.feat_mx_quantize(w, F32, None, 1, N, D, q, MX4, sq)
+        ctx.feat_mx_quantize(x, F32, None, B, T, D, a, MX4, sa)
+        s.wait_stream(side)
+        ctx.feat_mx_product(a, MX4, sa, q, sq, None, None, B, T, D, N, y, F32)
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.synchronize()
+    want = y.clone()
+    raw = [ref.dequantize(ref.unpacked(c.cpu().numpy(), "mx4"), sc.cpu().numpy(), "mx4", D) for c, sc in ((a, sa), (q, sq))]
+    exact = (raw[0] @ raw[1].T).reshape(B, T, N)
+    # sums in fp32 of D products: D steps of 2^-24 of the sum of their sizes at most
+    assert (np.abs(host(want) - exact) <= D * 2.0 ** -24 * (np.abs(raw[0]) @ np.abs(raw[1]).T).reshape(B, T, N)).all()
+    if captured:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            step()
+    for k in range(6):
+        with torch.cuda.stream(s):
+            for t in (a, sa, q, sq, y):
+                t.zero_()
+            g.replay() if captured else step()
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+
+
 def test_two_contexts_at_once():
     """Two streams, the same operators, nothing shared but the weights."""
     import torch
