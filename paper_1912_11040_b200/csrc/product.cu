@@ -425,12 +425,14 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
         bars->dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    chain_wait();                                        // nothing of memory has been touched so far
+    // Tensor memory is taken behind the wait: a kernel ahead that lets this one start before it has taken its own would find
+    // nothing left, and neither would end.
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&bars->tmem)),
                      "r"(TMEM_COLUMNS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    chain_wait();                                        // nothing of memory has been touched so far
     // which tiles have rows with values, a bit each, the same for every role
     for (int w = warp; w < LIVE_UNITS / 32 && 32 * w < u1 - u0; w += TILE_THREADS / 32) {
         const int u = u0 + 32 * w + lane;
