@@ -193,15 +193,17 @@ __device__ __forceinline__ void share_gains(float *to, const float *w, int D, in
 
 // Eight neighbours u of a row as codes: `codes` and `scales` are those of its first chunk of eight, and `chunk` this
 // one's number; four neighbouring threads hold a block and sixteen a group, whose scales the first of them writes.
+// A block wholly beyond the width D is zeros, although a norm that is not finite leaves NaN there (0 times it).  (No width, INT32_MAX,
+// for rows that have nothing but zeros there.)
 // All lanes of a warp take part, those without `on` for the shuffles alone.
 template <bool FOUR>
-__device__ __forceinline__ void store_chunk(const float *u, bool on, int chunk, uint8_t *codes, uint8_t *scales) {
+__device__ __forceinline__ void store_chunk(const float *u, bool on, int chunk, int D, uint8_t *codes, uint8_t *scales) {
     float a = fabsf(u[0]);
 #pragma unroll
     for (int i = 1; i < 7; i += 2) a = mx::max_abs(a, u[i], u[i + 1]);
     a = mx::max_abs(a, u[7], __shfl_xor_sync(~0u, mx::max_nan(a, fabsf(u[7])), 1));
     a = mx::max_nan(a, __shfl_xor_sync(~0u, a, 2));
-    const unsigned byte = mx::scale_byte(a, FOUR ? mx::EMAX_E2M1 : mx::EMAX_E4M3);
+    unsigned byte = mx::scale_byte(a, FOUR ? mx::EMAX_E2M1 : mx::EMAX_E4M3);
     const float inv = mx::inverse_scale(byte);
     float q[8];
 #pragma unroll
@@ -209,6 +211,7 @@ __device__ __forceinline__ void store_chunk(const float *u, bool on, int chunk, 
     if (__any_sync(~0u, byte == 255u)) {                 // blocks that are not finite: codes of zero
 #pragma unroll
         for (int i = 0; i < 8; ++i) q[i] = byte == 255u ? 0.f : q[i];
+        if (8 * (chunk & ~3) >= D) byte = 0;
     }
     unsigned s = byte;
     s |= __shfl_down_sync(~0u, s, 4) << 8;
@@ -316,7 +319,7 @@ rms_norm_kernel(const NormArgs a, const RowBatch batch) {
                     for (int c = 0; c < E / 8; ++c) {
                         const int chunk = c * TPR + l;
                         if (c * TPR < 16 * a.G)
-                            store_chunk<Y == AUG_ELEM_MX4>(v + 8 * c, valid && chunk < 16 * a.G, chunk, codes, scales);
+                            store_chunk<Y == AUG_ELEM_MX4>(v + 8 * c, valid && chunk < 16 * a.G, chunk, D, codes, scales);
                     }
                 } else {
 #pragma unroll
@@ -326,7 +329,7 @@ rms_norm_kernel(const NormArgs a, const RowBatch batch) {
                         const bool on = c + l < 16 * a.G;
                         float u[8] = {};
                         if (on) mx::load8(turned + 8 * (c + l), u);
-                        store_chunk<Y == AUG_ELEM_MX4>(u, on, c + l, codes, scales);
+                        store_chunk<Y == AUG_ELEM_MX4>(u, on, c + l, D, codes, scales);
                     }
                     P::meet();
                 }
@@ -555,7 +558,7 @@ mx_quantize_kernel(const T *x, uint8_t *codes, uint8_t *scales, int D, int G, in
                 __syncwarp();
                 mx::load8(turned[warp] + 8 * lane, v[r][c]);
             }
-            store_chunk<FOUR>(v[r][c], p.in[r] && chunk < 16 * G, chunk, codes + (int64_t)p.row[r] * G * (FOUR ? 64 : 128),
+            store_chunk<FOUR>(v[r][c], p.in[r] && chunk < 16 * G, chunk, INT32_MAX, codes + (int64_t)p.row[r] * G * (FOUR ? 64 : 128),
                               scales + (int64_t)p.row[r] * G * 4);
         }
 }

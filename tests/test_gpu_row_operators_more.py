@@ -1,0 +1,63 @@
+"""The operators on rows where they had not been looked at: more rows than the device holds at a time, eps beside squares at
+either end of fp32, codes of rows that are not finite, lengths at the ends of the product's tiles."""
+import numpy as np
+import pytest
+
+import row_reference as ref
+from paper_1912_11040_b200 import binding
+from test_gpu_row_operators import (BF16, EPS, F32, HALF, MX4, MX8, U32, check_grad, check_norm, check_product, context, guarded, host,
+                                    on_device, rows, to_counts, torch_type)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    return context(max_batch=4096)
+
+
+# ----------------------------------------------------------------------------- norm to codes
+def check_norm_codes(ctx, B, T, D, counts, t, kind, residual, shift=0, seed=0, spoil=None):
+    """Sum, codes and scales against the sum and the fp32 norm quantised, those against 64 bits."""
+    import torch
+    rng = np.random.default_rng(seed)
+    x = rows(rng, B, T, D, counts, t)
+    r = rows(rng, B, T, D, counts, t) if residual else None
+    if spoil:
+        spoil(x)
+    w = rng.normal(size=D).astype(np.float32)
+    c, ok = to_counts(counts), ref.holds(counts, B, T)
+    args = (on_device(x, t, shift), on_device(r, t, shift) if residual else None, t, torch.from_numpy(w).cuda(), c, B, T, D, EPS)
+    y = torch.empty(B, T, D, device="cuda")
+    sums = [guarded((B, T, D), torch_type(t), 3.0, shift) if residual else (None, lambda: True) for _ in range(2)]
+    size = (B, T, binding.feat_mx_code_bytes(kind, D)), (B, T, binding.feat_mx_scale_bytes(D))
+    out = [[guarded(s, torch.uint8, 0xAB) for s in size] for _ in range(2)]
+    ctx.feat_rms_norm(*args, sums[0][0], y, F32)
+    ctx.feat_mx_quantize(y, F32, c, B, T, D, out[0][0][0], kind, out[0][1][0])
+    ctx.feat_rms_norm(*args, sums[1][0], out[1][0][0], kind, out[1][1][0])
+    torch.cuda.synchronize()
+    with np.errstate(invalid="ignore"):             # (infinity times zero)
+        h, want = ref.rms_norm(x, r, w, EPS)
+    good = ok & np.isfinite(want).all(-1)
+    # the sum of squares, 1/sqrt and the products as in check_norm
+    assert np.all(np.abs(host(y) - want)[good] <= (np.abs(want) * (41 * U32))[good])
+    for s, intact in sums:
+        if residual:
+            assert np.all(np.abs(host(s) - h)[good] <= (np.abs(h) * (U32 + HALF[t]))[good]) and intact()
+    for a, b in zip(*out):
+        assert torch.equal(a[0], b[0]) and a[1]() and b[1]()
+    codes, scales = (v[0].cpu().numpy() for v in out[1])
+    beyond = -(-D // ref.BLOCK)
+    assert not scales[..., beyond:].any() and not codes[~ok].any() and not scales[~ok].any()
+    return scales, ok
+
+
+@pytest.mark.parametrize("D", [8, 40, 100, 128, 129, 257, 264, 640, 1000, 1025, 4100])
+@pytest.mark.parametrize("kind", [MX8, MX4])
+@pytest.mark.parametrize("t,shift", [(F32, 0), (BF16, 0), (BF16, 1)])
+def test_norm_to_codes_of_what_is_not_finite(ctx, D, kind, t, shift):
+    """Blocks that lie wholly beyond the width are zeros with a scale byte of 0, whatever the row holds."""
+    def spoil(x):
+        x[0, 0, 3], x[0, 1, -1], x[0, 2, 0], x[2, 1, D // 2] = np.nan, np.inf, -np.inf, np.nan
+    scales, ok = check_norm_codes(ctx, 3, 4, D, [4, 0, 2], t, kind, False, shift, D, spoil)
+    assert (scales[0, 0, : -(-D // ref.BLOCK)] == 255).all() and (scales[0, 3, : -(-D // ref.BLOCK)] != 255).all()
