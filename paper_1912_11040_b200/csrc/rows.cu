@@ -299,13 +299,14 @@ rms_norm_kernel(const NormArgs a, const RowBatch batch) {
         // threads of rows that share a warp stay together
         if (TPR < 32 || valid) {
             const float ss = P::sum(squares<E>(v, 1.f), 0.f, red, turn).x;
-            float rs = reciprocal_sqrt(fmaf(ss, a.inv_D, a.eps));
-            // squares beyond fp32 (or values that are not finite): once more, scaled down
-            const bool big = !(ss <= FLT_MAX);
+            const float mean = fmaf(ss, a.inv_D, a.eps);
+            float rs = reciprocal_sqrt(mean);
+            // squares beyond fp32, alone or with eps (or values that are not finite): once more, scaled down, eps with them
+            const bool big = !(mean <= FLT_MAX);
             if (TPR <= 32 ? __any_sync(~0u, big) : big) {
                 constexpr float DOWN = 0x1p-96f;
                 const float s2 = P::sum(squares<E>(v, DOWN), 0.f, red, turn).x;
-                if (big) rs = reciprocal_sqrt(s2 * a.inv_D) * DOWN;
+                if (big) rs = reciprocal_sqrt(fmaf(s2, a.inv_D, a.eps * DOWN * DOWN)) * DOWN;
             }
             if (a.sum && valid) P::store(static_cast<T *>(a.sum) + at, l, D, v);
 #pragma unroll

@@ -61,3 +61,17 @@ def test_norm_to_codes_of_what_is_not_finite(ctx, D, kind, t, shift):
         x[0, 0, 3], x[0, 1, -1], x[0, 2, 0], x[2, 1, D // 2] = np.nan, np.inf, -np.inf, np.nan
     scales, ok = check_norm_codes(ctx, 3, 4, D, [4, 0, 2], t, kind, False, shift, D, spoil)
     assert (scales[0, 0, : -(-D // ref.BLOCK)] == 255).all() and (scales[0, 3, : -(-D // ref.BLOCK)] != 255).all()
+
+
+# ----------------------------------------------------------------------------- eps at the ends of fp32
+@pytest.mark.parametrize("D", [1, 8, 40, 257, 1024, 4096, 10001])
+@pytest.mark.parametrize("scale,eps", [(2e18, 1e37), (1e19, 1e38), (1e19, 3e38), (3e19, 1e36), (1e20, 1.0)])
+def test_norm_with_eps_beside_squares_beyond_fp32(ctx, D, scale, eps):
+    import torch
+    rng = np.random.default_rng(D)
+    x = host(torch.from_numpy(scale * rng.uniform(0.5, 1.5, (5, D))).float())
+    y = torch.full((5, D), 3.0, device="cuda")
+    ctx.feat_rms_norm(on_device(x, F32), None, F32, None, None, 1, 5, D, eps, None, y, F32)
+    want = ref.rms_norm(x, None, None, float(np.float32(eps)))[1]
+    # as in check_norm; the scaling is by powers of two
+    assert np.all(np.abs(host(y) - want) <= np.abs(want) * (41 * U32))
