@@ -355,8 +355,9 @@ int64_t feat_mx_scale_bytes(int D);
  *   weight_dev [D] fp32, or NULL for ones
  *   y_dev   y_type: AUG_ELEM_F32 or AUG_ELEM_BF16, [B][T_max][D], or microscaled codes, with scales_dev
  *           (NULL otherwise)
- * eps > 0; D <= AUG_MAX_NORM_WIDTH, else AUG_ECAP.  sum_dev may be x_dev or residual_dev, and y_dev may be
- * either, where y_type is in_type and it is not sum_dev (else AUG_EINVAL). */
+ * eps is finite and at least 2^-126, the smallest normal number (else AUG_EINVAL); D <= AUG_MAX_NORM_WIDTH, else
+ * AUG_ECAP.  sum_dev may be x_dev or residual_dev, and y_dev may be either, where y_type is in_type and it is not
+ * sum_dev (else AUG_EINVAL). */
 int feat_rms_norm(AugCtx *ctx, const void *x_dev, const void *residual_dev, int in_type,
                   const float *weight_dev, const int *frame_counts_dev, int B, int T_max, int D, float eps,
                   void *sum_dev, void *y_dev, int y_type, uint8_t *scales_dev);
@@ -367,7 +368,7 @@ int feat_rms_norm(AugCtx *ctx, const void *x_dev, const void *residual_dev, int 
  *   dweight[D] = sum over all rows that hold values of dy h r, fp32, always written
  *   partial_dev   feat_rms_norm_partial_floats(D) floats for the call's use
  * The additions have a fixed order: the same inputs give the same bits.  dx_dev may be h_dev, dy_dev or dsum_dev.
- * Squares are summed in fp32 without scaling: |h| < 1e17. */
+ * eps as for the norm.  Squares are summed in fp32 without scaling: |h| < 1e17. */
 int feat_rms_norm_grad(AugCtx *ctx, const void *h_dev, const void *dy_dev, const void *dsum_dev, int type,
                        const float *weight_dev, const int *frame_counts_dev, int B, int T_max, int D,
                        float eps, void *dx_dev, float *dweight_dev, float *partial_dev);

@@ -734,6 +734,10 @@ struct LaunchGrad {
     int by_width() const { return grad_by_width<T, VEC>(a.D, *this); }
 };
 
+// Below the smallest normal number squares that underflow would count beside eps, and 1 / (mean + eps) would overflow in the
+// gradient of a row of zeros (0 times it is NaN).
+bool is_eps(float eps) { return eps >= FLT_MIN && eps <= FLT_MAX; }
+
 template <typename F>
 int by_type(int type, bool vec, const F &f) {
     if (type == AUG_ELEM_F32) return vec ? f.template by_width<float, true>() : f.template by_width<float, false>();
@@ -789,7 +793,7 @@ int feat_rms_norm(AugCtx *ctx, const void *x_dev, const void *residual_dev, int 
     const int rc = check_rows(ctx, frame_counts_dev, B, T_max, D, &none);
     if (rc != AUG_OK || none) return rc;
     if (!x_dev || !y_dev || !is_row_type(in_type) || !(is_row_type(y_type) || is_mx_type(y_type))) return AUG_EINVAL;
-    if (!(eps > 0.f) || !(eps <= FLT_MAX)) return AUG_EINVAL;
+    if (!is_eps(eps)) return AUG_EINVAL;
     if (is_mx_type(y_type) != (scales_dev != nullptr)) return AUG_EINVAL;
     if (D > MAX_WIDTH) return AUG_ECAP;
     // an output over an input of another width, or two outputs in one place, would be written while rows are still read
@@ -821,7 +825,7 @@ int feat_rms_norm_grad(AugCtx *ctx, const void *h_dev, const void *dy_dev, const
     if (!dweight_dev || (uintptr_t)dweight_dev & 3) return AUG_EINVAL;
     if (none) return cudaMemsetAsync(dweight_dev, 0, sizeof(float) * D, ctx->stream) == cudaSuccess ? AUG_OK : AUG_ECUDA;
     if (!h_dev || !dy_dev || !dx_dev || !partial_dev || !is_row_type(type)) return AUG_EINVAL;
-    if (!(eps > 0.f) || !(eps <= FLT_MAX)) return AUG_EINVAL;
+    if (!is_eps(eps)) return AUG_EINVAL;
     const uintptr_t rows_at = (uintptr_t)h_dev | (uintptr_t)dy_dev | (uintptr_t)dsum_dev | (uintptr_t)dx_dev;
     if (rows_at & (elem_bytes(type) - 1) || ((uintptr_t)weight_dev | (uintptr_t)partial_dev) & 3) return AUG_EINVAL;
     const bool vec = (D & 7) == 0 && (rows_at & 15) == 0;

@@ -75,3 +75,36 @@ def test_norm_with_eps_beside_squares_beyond_fp32(ctx, D, scale, eps):
     want = ref.rms_norm(x, None, None, float(np.float32(eps)))[1]
     # as in check_norm; the scaling is by powers of two
     assert np.all(np.abs(host(y) - want) <= np.abs(want) * (41 * U32))
+
+
+LEAST = 2.0 ** -126                     # the smallest normal number of fp32
+
+
+@pytest.mark.parametrize("D", [8, 40, 257, 1024])
+def test_smallest_eps(ctx, D):
+    """Squares lose what lies below 2^-149 of them, which is 2^-24 of the smallest eps at most."""
+    import torch
+    rng = np.random.default_rng(D)
+    h = rng.normal(size=(6, D)) * np.array([0.0, 1e-21, 1e-19, 3e-19, 1e-15, 1.0])[:, None]
+    h = host(torch.from_numpy(h).float())
+    dy = host(torch.from_numpy(rng.normal(size=(6, D))).float())
+    y, dx = (torch.full((6, D), 3.0, device="cuda") for _ in range(2))
+    dw, part = torch.empty(D, device="cuda"), torch.empty(binding.feat_rms_norm_partial_floats(D), device="cuda")
+    ctx.feat_rms_norm(on_device(h, F32), None, F32, None, None, 1, 6, D, LEAST, None, y, F32)
+    ctx.feat_rms_norm_grad(on_device(h, F32), on_device(dy, F32), None, F32, None, None, 1, 6, D, LEAST, dx, dw, part)
+    want = ref.rms_norm(h, None, None, LEAST)[1]
+    # as in check_norm, and the mean of squares off by two more units: what each square loses, and the mean itself
+    assert np.all(np.abs(host(y) - want) <= np.abs(want) * (43 * U32))
+    dx_want, dw_want, size, dw_size = ref.rms_norm_grad(h, dy, None, None, LEAST)
+    assert np.all(np.abs(host(dx) - dx_want) <= size * (94 * U32))       # as in check_grad, and the same two, twice
+    assert np.all(np.abs(host(dw) - dw_want) <= dw_size * (6 + 440 + 3) * U32)
+
+
+@pytest.mark.parametrize("eps", [2.0 ** -127, 1e-40, 2.0 ** -149])
+def test_eps_below_the_smallest_normal_number_is_refused(ctx, eps):
+    import torch
+    x, dx = torch.zeros(2, 64, device="cuda"), torch.full((2, 64), 3.0, device="cuda")
+    dw, part = torch.full((64,), 3.0, device="cuda"), torch.empty(binding.feat_rms_norm_partial_floats(64), device="cuda")
+    assert ctx.feat_rms_norm(x, None, F32, None, None, 1, 2, 64, eps, None, dx, F32, check=False) == binding.AUG_EINVAL
+    assert ctx.feat_rms_norm_grad(x, x, None, F32, None, None, 1, 2, 64, eps, dx, dw, part, check=False) == binding.AUG_EINVAL
+    assert (dx == 3).all() and (dw == 3).all()
