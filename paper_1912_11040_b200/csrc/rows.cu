@@ -174,12 +174,19 @@ __device__ __forceinline__ float reciprocal_sqrt(float x) {
     const float r = rsqrtf(x), e = fmaf(-x * r, r, 1.f);
     return x <= FLT_MAX ? fmaf(0.5f * r, e, r) : r;
 }
-// Sum of squares in four parts
+// Sums of squares and of products in four parts
 template <int E>
 __device__ __forceinline__ float squares(const float *v, float scale) {
     float s[4] = {};
 #pragma unroll
     for (int e = 0; e < E; ++e) s[e & 3] = fmaf(v[e] * scale, v[e] * scale, s[e & 3]);
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+template <int E>
+__device__ __forceinline__ float products(const float *u, const float *v) {
+    float s[4] = {};
+#pragma unroll
+    for (int e = 0; e < E; ++e) s[e & 3] = fmaf(u[e], v[e], s[e & 3]);
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
@@ -409,16 +416,10 @@ rms_norm_grad_kernel(const GradArgs a, const RowBatch batch) {
         if (AHEAD) read(at + (int64_t)step * D, next);
         const bool later = batch.holds(row + 2 * step);
         if (TPR < 32 || valid) {
-            float ss = 0.f, dot = 0.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) g[e] = dy[e];
             if (a.w) P::scale(g, gains, a.w, l, D);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                ss = fmaf(h[e], h[e], ss);
-                dot = fmaf(g[e], h[e], dot);
-            }
-            const float2 both = P::sum(ss, dot, red, turn);
+            const float2 both = P::sum(products<E>(h, h), products<E>(g, h), red, turn);
             const float rs = reciprocal_sqrt(fmaf(both.x, a.inv_D, a.eps)), c = rs * rs * (both.y * a.inv_D);
 #pragma unroll
             for (int e = 0; e < E; ++e) {

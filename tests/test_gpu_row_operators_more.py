@@ -108,3 +108,21 @@ def test_eps_below_the_smallest_normal_number_is_refused(ctx, eps):
     assert ctx.feat_rms_norm(x, None, F32, None, None, 1, 2, 64, eps, None, dx, F32, check=False) == binding.AUG_EINVAL
     assert ctx.feat_rms_norm_grad(x, x, None, F32, None, None, 1, 2, 64, eps, dx, dw, part, check=False) == binding.AUG_EINVAL
     assert (dx == 3).all() and (dw == 3).all()
+
+
+# ----------------------------------------------------------------------------- the gradient's sums
+def test_sums_of_the_gradient_are_in_four_parts(ctx):
+    """A thread has sixteen neighbours by eights.  Of each sixteen the first value is 1 and the others are 2^-12, whose squares are
+    half a unit of it: behind it in one sum all fifteen are lost, in four parts three."""
+    import torch
+    D, eps = 1024, 2.0 ** -20
+    h = torch.full((1, D), 2.0 ** -12, device="cuda")
+    h[0, 0:512:8] = 1.0
+    h, one = h.bfloat16(), torch.ones(1, D, device="cuda").bfloat16()
+    dx, dw = torch.empty_like(h), torch.empty(D, device="cuda")
+    part = torch.empty(binding.feat_rms_norm_partial_floats(D), device="cuda")
+    ctx.feat_rms_norm_grad(h, one, None, BF16, None, None, 1, 1, D, eps, dx, dw, part)
+    want = ref.rms_norm_grad(host(h), np.ones((1, D)), None, None, eps)[1]
+    # the parts lose 3 U32 of the sum, the sums of threads are exact, the mean with eps is one U32: halved by the square
+    # root, which is good to 2 U32 (its last bit but one); h and dy are powers of two
+    assert np.all(np.abs(host(dw) - want) <= np.abs(want) * ((3 + 1) / 2 + 2) * U32)
