@@ -126,3 +126,69 @@ def test_sums_of_the_gradient_are_in_four_parts(ctx):
     # the parts lose 3 U32 of the sum, the sums of threads are exact, the mean with eps is one U32: halved by the square
     # root, which is good to 2 U32 (its last bit but one); h and dy are powers of two
     assert np.all(np.abs(host(dw) - want) <= np.abs(want) * ((3 + 1) / 2 + 2) * U32)
+
+
+# ----------------------------------------------------------------------------- more rows than the device holds at a time
+def some_counts(B, T, seed):
+    return [int(c) for c in np.random.default_rng(seed).integers(-1, T + 2, B)]
+
+
+MANY = [(4000, 15, 40), (2400, 15, 128), (2000, 12, 257), (800, 15, 1024), (300, 10, 4100), (100, 10, 8192), (60, 10, 16384)]
+
+
+@pytest.mark.parametrize("B,T,D", MANY)
+@pytest.mark.parametrize("t,yt", [(F32, F32), (BF16, BF16)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_norm_of_many_rows(ctx, B, T, D, t, yt, shift):
+    check_norm(ctx, B, T, D, [max(c, 0) for c in some_counts(B, T, D)], t, yt, shift=shift)
+
+
+@pytest.mark.parametrize("B,T,D", MANY)
+@pytest.mark.parametrize("t,kind,shift", [(F32, MX4, 0), (F32, MX8, 1), (BF16, MX8, 0), (BF16, MX4, 1)])
+def test_norm_of_sums_to_codes(ctx, B, T, D, t, kind, shift):
+    check_norm_codes(ctx, B, T, D, some_counts(B, T, D), t, kind, True, shift)
+
+
+@pytest.mark.parametrize("D", [8, 40, 128, 136, 257, 384, 512, 640, 768, 1000, 1024, 1536, 2048, 2050, 4096, 4100, 8192])
+@pytest.mark.parametrize("kind", [MX8, MX4])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_norm_of_few_sums_to_codes(ctx, D, kind, shift):
+    for t in (F32, BF16):
+        check_norm_codes(ctx, 3, 4, D, [4, 0, 3], t, kind, True, shift, D)
+
+
+@pytest.mark.parametrize("B,T,D", [(4000, 15, 40), (4000, 10, 80), (2400, 15, 128), (2000, 8, 257), (600, 10, 1024), (100, 8, 4100),
+                                   (60, 10, 10001)])
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_grad_of_many_rows(ctx, B, T, D, t, shift):
+    check_grad(ctx, B, T, D, some_counts(B, T, D), t, shift=shift)
+
+
+@pytest.mark.parametrize("B,T,D", [(4000, 15, 40), (4000, 10, 80), (2400, 15, 128), (2000, 8, 257), (600, 10, 1024), (100, 8, 4100),
+                                   (60, 10, 10001)])
+@pytest.mark.parametrize("t", [F32, BF16])
+def test_grad_of_the_weights_counts_every_row_once(ctx, B, T, D, t):
+    """h = +-1 and eps = 3, so that mean(h^2) + eps is 4 (the nearest number to it, whatever 1 / D is rounded to) and n is h / 2;
+    whole numbers as dy: all terms are multiples of 1/2 whose sums stay below 2^23, so that dw is exact."""
+    import torch
+    rng = np.random.default_rng(D)
+    counts = some_counts(B, T, D)
+    ok = ref.holds(counts, B, T)
+    h, dy = rng.choice([-1.0, 1.0], (B, T, D)), rng.integers(-8, 9, (B, T, D)).astype(float)
+    want = (dy * h * ok[..., None]).sum((0, 1)) / 2
+    h[~ok], dy[~ok] = np.nan, np.nan
+    dx, dw = torch.empty(B, T, D, dtype=torch_type(t), device="cuda"), torch.empty(D, device="cuda")
+    part = torch.empty(binding.feat_rms_norm_partial_floats(D), device="cuda")
+    ctx.feat_rms_norm_grad(on_device(h, t), on_device(dy, t), None, t, None, to_counts(counts), B, T, D, 3.0, dx, dw, part)
+    assert np.array_equal(host(dw), want)
+
+
+# ----------------------------------------------------------------------------- the product's longest rows
+@pytest.mark.parametrize("kind,K", [(MX4, 2304), (MX4, 2305), (MX4, 4353), (MX4, 6913), (MX4, 11776), (MX4, 11777), (MX4, 13312), (MX4, 13313),
+                                    (MX8, 1152), (MX8, 1153), (MX8, 2305), (MX8, 3841), (MX8, 7040), (MX8, 7041), (MX8, 7808),
+                                    (MX8, 7809)])
+@pytest.mark.parametrize("N,t", [(16, BF16), (200, F32)])
+def test_product_at_the_ends_of_its_tiles(ctx, kind, K, N, t):
+    """Where tiles get narrower for the length of the rows, and where the rows go another way."""
+    check_product(ctx, 1, 140, K, N, None, kind, t, seed=K + N)
