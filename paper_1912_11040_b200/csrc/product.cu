@@ -814,8 +814,8 @@ bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool
     double least = 0;
     bool found = false;
     int last = 0;
-    // (a row's scales are fetched by their number among all, which has to be an int)
-    if (KS > MAX_KS || (int64_t)rows * p.G > INT32_MAX) return false;
+    // (scales are fetched by their number among all, which has to be an int, for rows of the last tile beyond the batch, too)
+    if (KS > MAX_KS || (int64_t)MT * TILE_M * p.G > (int64_t)INT32_MAX + 1) return false;
     for (int tiles = (p.N + MAX_NT - 1) / MAX_NT; tiles <= (p.N + 15) / 16; ++tiles) {
         TilePlan t;
         const int wide = tiles == 1 || !whole ? 16 : p.bf16_out ? 64 : 32;
