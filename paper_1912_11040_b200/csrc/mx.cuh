@@ -10,7 +10,7 @@
 
 namespace mx {
 
-constexpr int BLOCK = 32, GROUP = 128;
+constexpr int GROUP = 128;
 constexpr int EMAX_E4M3 = 8, EMAX_E2M1 = 2;      // exponents of the formats' largest numbers
 
 inline __host__ __device__ int groups(int D) { return (int)(((unsigned)D + GROUP - 1) / GROUP); }

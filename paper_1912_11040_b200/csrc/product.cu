@@ -11,7 +11,7 @@ struct ProductArgs {
     const uint8_t *a, *a_scales, *w, *w_scales;
     const float *bias;
     void *out;
-    int K, G, N;           // G: groups of 128 along K
+    int G, N;              // groups of 128 along K, columns
     bool bf16_out;
     float pad;
 };
@@ -930,7 +930,7 @@ extern "C" int feat_mx_product(AugCtx *ctx, const uint8_t *a_codes_dev, int a_ty
     if (!on16(a_codes_dev) || !on16(a_scales_dev) || !on16(w_codes_dev) || !on16(w_scales_dev)) return AUG_EINVAL;
     if ((uintptr_t)bias_dev & 3 || (uintptr_t)out_dev & (elem_bytes(out_type) - 1)) return AUG_EINVAL;
     if (K > AUG_MAX_PRODUCT_WIDTH || N > AUG_MAX_PRODUCT_WIDTH) return AUG_ECAP;
-    const ProductArgs p = {a_codes_dev, a_scales_dev, w_codes_dev, w_scales_dev, bias_dev, out_dev, K, mx::groups(K), N,
+    const ProductArgs p = {a_codes_dev, a_scales_dev, w_codes_dev, w_scales_dev, bias_dev, out_dev, mx::groups(K), N,
                            out_type == AUG_ELEM_BF16, ctx->cfg.pad_value};
     const RowBatch batch(frame_counts_dev, T_max, B);
     const bool a4 = a_type == AUG_ELEM_MX4;

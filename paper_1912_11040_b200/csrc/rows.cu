@@ -638,11 +638,10 @@ int norm_by_width(int D, F f) {
         if (D <= 64) return f.template operator()<T, 8, 8, VEC>();
         if (D <= 128) return f.template operator()<T, 8, 16, VEC>();
     }
-    if constexpr (VEC) {
+    if constexpr (VEC && CODES)
         if (D <= 128) return f.template operator()<T, 16, 8, VEC>();
-    } else {
+    if constexpr (!VEC)
         if (D <= 128) return f.template operator()<T, 32, 4, VEC>();
-    }
     if (D <= 256) return f.template operator()<T, 32, 8, VEC>();
     if constexpr (!VEC)
         if (D <= 384) return f.template operator()<T, 32, 12, VEC>();
