@@ -184,6 +184,82 @@ def test_grad_of_the_weights_counts_every_row_once(ctx, B, T, D, t):
     assert np.array_equal(host(dw), want)
 
 
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("B,T,D", [(4000, 15, 40), (2000, 12, 257), (800, 15, 1024), (60, 10, 16384)])
+def test_many_rows_in_place(ctx, B, T, D, t):
+    """Rows that are read ahead are not those that are written meanwhile."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    new = lambda: torch.randn(B, T, D, device="cuda", generator=gen).to(torch_type(t))
+    x, r, w = new(), new(), torch.randn(D, device="cuda", generator=gen)
+    c = to_counts(some_counts(B, T, D))
+    y, s, y0, s0 = (torch.empty_like(x) for _ in range(4))
+    ctx.feat_rms_norm(x, r, t, w, c, B, T, D, EPS, s, y, t)
+    ctx.feat_rms_norm(x, None, t, w, c, B, T, D, EPS, s0, y0, t)            # a sum of one
+    ok = torch.arange(T, device="cuda")[None, :] < c[:, None]
+    assert torch.equal(s0[ok], x[ok])
+    x1, r1 = x.clone(), r.clone()
+    ctx.feat_rms_norm(x1, r1, t, w, c, B, T, D, EPS, r1, x1, t)
+    assert torch.equal(x1, y) and torch.equal(r1, s)
+    x1 = x.clone()
+    ctx.feat_rms_norm(x1, None, t, w, c, B, T, D, EPS, None, x1, t)
+    assert torch.equal(x1, y0)
+    part = torch.empty(binding.feat_rms_norm_partial_floats(D), device="cuda")
+    dx, dw, dw1, ds = torch.empty_like(x), torch.empty(D, device="cuda"), torch.empty(D, device="cuda"), new()
+    ctx.feat_rms_norm_grad(x, r, ds, t, w, c, B, T, D, EPS, dx, dw, part)
+    for k in range(3):
+        v = [x.clone(), r.clone(), ds.clone()]
+        ctx.feat_rms_norm_grad(*v, t, w, c, B, T, D, EPS, v[k], dw1, part)
+        assert torch.equal(v[k], dx) and torch.equal(dw1, dw)
+
+
+def test_more_values_than_an_int_counts():
+    """2^21 rows and some of 1024 values: the last rows begin beyond 2^31 values (beyond 2^32 bytes of any type but codes)."""
+    import torch
+    D, N, T = 1024, 1024, (1 << 21) + 300
+    ctx = context(max_batch=1)
+    at = [0, 1, 148 * 7, (1 << 20) - 1, 1 << 20, (1 << 21) - 1, 1 << 21, (1 << 21) + 127, T - 2, T - 1]
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.empty(T, D, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    gain = 1 + 0.1 * torch.randn(D, device="cuda", generator=gen)
+    y = torch.empty_like(x)
+    ctx.feat_rms_norm(x, None, BF16, gain, None, 1, T, D, EPS, None, y, BF16)
+    some, w = host(x[at]), host(gain)
+    want = ref.rms_norm(some, None, w, EPS)[1]
+    assert np.all(np.abs(host(y[at]) - want) <= np.abs(want) * (40 * U32 + HALF[BF16]))
+    codes = torch.empty(T, binding.feat_mx_code_bytes(MX8, D), dtype=torch.uint8, device="cuda")
+    scales = torch.empty(T, binding.feat_mx_scale_bytes(D), dtype=torch.uint8, device="cuda")
+    ctx.feat_rms_norm(x, None, BF16, gain, None, 1, T, D, EPS, None, codes, MX8, scales)
+    normed = [c[at].clone() for c in (codes, scales)]
+    f = torch.empty(len(at), D, device="cuda")
+    few = [torch.empty_like(c) for c in normed]
+    ctx.feat_rms_norm(x[at].contiguous(), None, BF16, gain, None, 1, len(at), D, EPS, None, f, F32)
+    ctx.feat_mx_quantize(f, F32, None, 1, len(at), D, few[0], MX8, few[1])
+    assert all(torch.equal(a, b) for a, b in zip(normed, few))
+    ctx.feat_mx_quantize(x, BF16, None, 1, T, D, codes, MX8, scales)
+    raw_c, raw_s = ref.quantize(some, "mx8")
+    got_c, got_s = codes[at].cpu().numpy(), scales[at].cpu().numpy()
+    assert np.array_equal(got_s, raw_s) and np.array_equal(np.where(got_c == 128, 0, got_c), np.where(raw_c == 128, 0, raw_c))
+    a = ref.dequantize(got_c, got_s, "mx8", D)
+    ctx.feat_mx_dequantize(codes, MX8, scales, None, 1, T, D, y, BF16)
+    assert np.all(np.abs(host(y[at]) - a) <= np.abs(a) * HALF[BF16])
+    w_codes = torch.empty(N, binding.feat_mx_code_bytes(MX4, D), dtype=torch.uint8, device="cuda")
+    w_scales = torch.empty(N, binding.feat_mx_scale_bytes(D), dtype=torch.uint8, device="cuda")
+    ctx.feat_mx_quantize(torch.randn(N, D, device="cuda", generator=gen), F32, None, 1, N, D, w_codes, MX4, w_scales)
+    ctx.feat_mx_product(codes, MX8, scales, w_codes, w_scales, None, None, 1, T, D, N, y, BF16)
+    wv = ref.dequantize(ref.unpacked(w_codes.cpu().numpy(), "mx4"), w_scales.cpu().numpy(), "mx4", D)
+    want, size = a @ wv.T, np.abs(a) @ np.abs(wv).T
+    assert np.all(np.abs(host(y[at]) - want) <= size * ((D + 1) * 2 * U32) + np.abs(want) * HALF[BF16])
+    out = torch.empty(T, N - 1, dtype=torch.bfloat16, device="cuda")         # rows that start anywhere
+    ctx.feat_mx_product(codes, MX8, scales, w_codes, w_scales, None, None, 1, T, D, N - 1, out, BF16)
+    assert torch.equal(out[at], y[at][:, :-1])
+    dx, dw, part = torch.empty_like(x), torch.empty(D, device="cuda"), torch.empty(binding.feat_rms_norm_partial_floats(D), device="cuda")
+    ctx.feat_rms_norm_grad(x, y, None, BF16, gain, None, 1, T, D, EPS, dx, dw, part)
+    dx_want, _, size, _ = ref.rms_norm_grad(some, host(y[at]), None, w, EPS)
+    assert np.all(np.abs(host(dx[at]) - dx_want) <= size * (90 * U32) + np.abs(dx_want) * HALF[BF16])
+    assert ctx.aug_last_status() == (-1, 0)
+
+
 # ----------------------------------------------------------------------------- the product's longest rows
 @pytest.mark.parametrize("kind,K", [(MX4, 2304), (MX4, 2305), (MX4, 4353), (MX4, 6913), (MX4, 11776), (MX4, 11777), (MX4, 13312), (MX4, 13313),
                                     (MX8, 1152), (MX8, 1153), (MX8, 2305), (MX8, 3841), (MX8, 7040), (MX8, 7041), (MX8, 7808),
