@@ -320,8 +320,9 @@ int aug_bucket_by_length(const int *lengths_host, int B, int batch, int *perm_ho
  *     matter; they receive pad_value, or zeros where codes or gradients are written.
  *   - Rows are fp32 or bf16 (AugElem) and aligned to their element; 16-byte aligned rows whose width
  *     is a multiple of 8 are read and written with 128-bit accesses and are faster.
- *   - B * T_max <= AUG_MAX_ROWS, else AUG_ECAP.  An output may be the very buffer of an input of the
- *     same type where that is said; buffers that overlap in any other way give undefined results.
+ *   - B <= max_batch of the context and B * T_max <= AUG_MAX_ROWS, else AUG_ECAP.  An output may be
+ *     the very buffer of an input of the same type where that is said; buffers that overlap in any
+ *     other way give undefined results.
  *   - They use no workspace of the context: calls on different contexts, and graphs captured from
  *     them, share nothing but the caller's buffers.
  *
@@ -368,7 +369,8 @@ int feat_rms_norm(AugCtx *ctx, const void *x_dev, const void *residual_dev, int 
  *   dweight[D] = sum over all rows that hold values of dy h r, fp32, always written
  *   partial_dev   feat_rms_norm_partial_floats(D) floats for the call's use
  * The additions have a fixed order: the same inputs give the same bits.  dx_dev may be h_dev, dy_dev or dsum_dev.
- * eps as for the norm.  Squares are summed in fp32 without scaling: |h| < 1e17. */
+ * eps as for the norm.  Sums over a row are taken in fp32 without scaling: |h| < 1e17, and the sum of |weight dy h| below
+ * 1e38. */
 int feat_rms_norm_grad(AugCtx *ctx, const void *h_dev, const void *dy_dev, const void *dsum_dev, int type,
                        const float *weight_dev, const int *frame_counts_dev, int B, int T_max, int D,
                        float eps, void *dx_dev, float *dweight_dev, float *partial_dev);
@@ -388,7 +390,10 @@ int feat_mx_dequantize(AugCtx *ctx, const uint8_t *codes_dev, int mx_type, const
  *   w_codes_dev, w_scales_dev   N rows of width K, AUG_ELEM_MX4: quantised once, kept by the caller
  *   bias_dev [N] fp32 or NULL;  out_dev [B][T_max][N] of out_type (AUG_ELEM_F32 or AUG_ELEM_BF16)
  * K and N up to AUG_MAX_PRODUCT_WIDTH, else AUG_ECAP.  Codes and scales beyond K, up to the whole group, have to be
- * there and zero.  Products within a block are exact; sums over blocks are carried in fp32. */
+ * there and zero.  Products of elements are exact, their sums are carried in fp32.
+ * More than eight rows go by tiles whose weights stay on the chip for all of K, of fewer columns the longer the
+ * rows are: at full speed for K up to 2048 (AUG_ELEM_MX8: 1024).  Above about 11776 (7040) the weights are read
+ * again for every eight rows. */
 #define AUG_MAX_PRODUCT_WIDTH 16384
 int feat_mx_product(AugCtx *ctx, const uint8_t *a_codes_dev, int a_type, const uint8_t *a_scales_dev,
                     const uint8_t *w_codes_dev, const uint8_t *w_scales_dev, const float *bias_dev,

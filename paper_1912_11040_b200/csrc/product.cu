@@ -167,10 +167,10 @@ int launch_few_rows(AugCtx *ctx, const ProductArgs &p, const RowBatch &batch) {
 // multiprocessor works through a contiguous part of the tiles, ordered by columns first, so that it loads weights once
 // or twice and all CTAs pass the same rows at about the same time (they come from L2 after the first).
 //
-// 64 x 1998 rows (two thirds hold values), 1024 x 1024, out in 16 bits: 84 us, 2150 TFLOP/s.  The bytes would take 48, but nearly
-// all of them are written, and writes alone do not reach the copy's rate: a fill of the output takes 74 us, this kernel with K = 80
-// takes 58.  The rest is that the rows are read once for every 128 columns (54 bytes a clock is what a multiprocessor gets) while the
-// instructions of 128 columns take 95 clocks instead of 64.  In 8 bits the rows are twice as long, the weights leave
+// 64 x 1998 rows (two thirds hold values), 1024 x 1024, out in 16 bits: 84 us, 2150 TFLOP/s.  The bytes would take 48.  Nearly all of
+// them are written: with K = 80, which writes the same output, this kernel takes 57 us (bytes 41).  The rest is that the rows are read
+// once for every 128 columns (54 bytes a clock is what a multiprocessor gets) while the instructions of 128 columns take 95 clocks
+// instead of 64; the tensor pipe is busy for 31 % of the time, and nothing is saturated.  In 8 bits the rows are twice as long, the weights leave
 // room for four stages, and the wait for them is what counts: 159 us.
 //
 //   warp 0      fetches 128 rows x 128 bytes a stage with TMA, swizzled as the tensor cores read them, and the weights
@@ -805,8 +805,10 @@ tile_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
 }
 
 // Columns of a tile and what shared memory holds; false where there is no room for as few as that.  `whole`: tiles of whole
-// pieces, as everything is that has room for them (64 x 1998 x 1024 x 1024: tiles of 128 columns 112 us, of 144 148); others may
-// have any multiple of 16 columns.
+// pieces, which go by TMA, as everything is that has room for them; others may have any multiple of 16 columns, word by word
+// (64 x 1998 x 1024 rows, 1024 columns: 84 us and 136, 656 columns: 76 and 107).  The longer the rows, the fewer columns fit: with 16-bit
+// output of 1024 columns 128 up to K = 2304 (8-bit rows 1152), 64 up to 4352 (2304), 48 and 32 word by word up to 6912 (3840), 16
+// up to 11776 (7040).
 bool plan_tiles(const AugCtx *ctx, int rows, const ProductArgs &p, bool a4, bool whole, TilePlan *best) {
     const Out out = how_to_write(p, a4, whole);
     const int piece_bytes = 32 * (out == HALF ? 64 : 128);

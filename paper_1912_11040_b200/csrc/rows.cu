@@ -267,7 +267,7 @@ __device__ __forceinline__ void pad_row(const NormArgs &a, int row, int l) {
 // CTAs stay, and the next row (and whether the one after it holds values) is on its way while one is worked on.  The norm is
 // that of x + r in fp32, before the sum is rounded to be stored.
 //
-// 64 x 1998 rows of 1024 in 16 bits (two thirds of them hold values), residual and sum, to 8 bits: 133 us, the bytes take 116;
+// 64 x 1998 rows of 1024 in 16 bits (two thirds of them hold values), residual and sum, to 8 bits: 137 us, the bytes take 116;
 // 64 x 998 in fp32 140 of 136.  What kept it from that were instructions: with a branch for every value's column, rows that hold
 // nothing worked on like the others and the gains read a value at a time it was 177 (44 M warp instructions for 52 M values).
 template <typename T, int TPR, int E, bool VEC, int Y>
@@ -365,7 +365,7 @@ rms_norm_kernel(const NormArgs a, const RowBatch batch) {
 // on their way meanwhile, and every thread carries its columns' share of dw over all rows of its CTA.  The CTAs'
 // shares go to `partial`, and a second kernel adds them in a fixed order: no atomics, the same result every time.
 //
-// 64 x 998 rows of 1024 in 16 bits with dsum: 73 us, the bytes take 62.  With a row to a warp, 32 values a thread and nothing
+// 64 x 998 rows of 1024 in 16 bits with dsum: 72 us, the bytes take 62.  With a row to a warp, 32 values a thread and nothing
 // on its way it was 195: 206 registers left room for eight warps a multiprocessor, which waited for memory.
 struct GradArgs {
     const void *h, *dy, *dsum;
@@ -666,7 +666,9 @@ int norm_by_width(int D, F f) {
     return f.template operator()<T, 512, 32, VEC>();
 }
 // The gradient holds three rows and their successors, and the shares of dw: 64 x 1998 rows of 80 fp32 by sixteen threads 26 us,
-// and with the sixteen rows' shares of a CTA added one after the other 32.
+// and with the sixteen rows' shares of a CTA added one after the other 32.  The last kind, for rows above 4096 (in 16 bits on 16-byte
+// boundaries 8192), does not fit into the registers that 512 threads leave: 64 x 64 x 16384 with dsum 154 us in 16 bits (bytes 59) and
+// 233 in fp32 (118), 64 x 64 x 10001 without it 595 (28) and 272 (56).
 template <typename T, bool VEC, typename F>
 int grad_by_width(int D, F f) {
     constexpr bool WIDE = VEC && sizeof(T) == 2;
